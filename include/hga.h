@@ -579,6 +579,154 @@ hga_status hga_prefill_blocks(const hga_plan* plan, const void* q_blocks, int32_
  * c < 0. */
 int32_t hga_visible_chunks(const hga_params* params, int32_t c, int32_t* chunks, int32_t cap);
 
+/* ---- Single tokens over a paged 4-bit cache --------------------------------
+ *
+ * The serving form of the path: sequences of any lengths, each appended to a
+ * token at a time (or a prompt at a time), every token routed and attended by
+ * itself.  The chunks of a sequence are pages of a pool, found through a page
+ * table; page c of a sequence is its chunk c, positions [64 c, 64 c + 64).
+ *
+ * A page holds the keys and values of its 64 positions for every KV head, in
+ * 4 bits.  A row of head_dim values is head_dim/32 blocks of 32; a block's
+ * values are 4-bit codes, a sign (bit 3) and a magnitude (bits 0-2) of
+ * {0, 0.5, 1, 1.5, 2, 3, 4, 6}, times the block's scale 2^(e - 127), one byte
+ * e.  hga_cache_append takes the smallest scale under which the block's largest
+ * magnitude is at most 6 (e in [2, 253]) and rounds to the nearest value, ties
+ * to the even code (at e = 253 to at most 3, whose next would overflow); a
+ * block with a NaN or an infinity becomes e = 255, which stands for NaN.
+ * Bytes of a page: [n_kv_heads] of
+ *   64*d/2    key codes     row r, dimension j: byte r*d/2 + j/2, the low half
+ *                           for even j
+ *   64*d/2    value codes   [r/4][j / (d/16)][r%4][j % (d/16) / 2]
+ *   64*d/32   key scales    [r%16][j/32][r/16]
+ *   64*d/32   value scales  [r/4 % 4][j/32][r/16][r%4]
+ * (d = head_dim; d*17/16 bytes a position and head, against 4d of bf16.)
+ *
+ * The pool.  Page ids [0, n_pages) lie in device memory, ids
+ * [n_pages, n_pages + n_cold) in the cold tier, pinned host memory that the
+ * kernels read and write over the host link (Sec. 4.3); the summaries of all
+ * of them lie in device memory, so routing never crosses the link.  Any other
+ * id in a page table marks an absent page: its positions are not seen, not
+ * listed, not written.
+ *   pages     device [n_layers][n_pages][hga_page_bytes]
+ *   cold      pinned host [n_layers][n_cold][hga_page_bytes], or NULL
+ *   page_sum  device fp32 [n_layers][n_pages + n_cold][n_kv_heads][head_dim]:
+ *             the mean of a full page's stored keys turned to the page's
+ *             middle (chunk_sum of hga_build_summaries, of the keys as
+ *             stored); hga_cache_append writes it when a page fills
+ *
+ * The tokens of a call, in any mixture of sequences: token t is position
+ * tok_pos[t] of sequence tok_seq[t].  A token whose sequence or position lies
+ * outside the table is idle (a padded batch marks its empty slots so).
+ * page_table is [n_seqs][max_pages], max_pages <= 2^18.  What is read of these
+ * device arrays is checked by the kernels: no id leads outside the pool.
+ *
+ * The plan gives heads, head_dim, dtype, the rotary phases and the routing
+ * parameters (keep_first, keep_last, force_prev, topk_chunks); its batch and
+ * topk_groups play no part.  Rows of q, k and v may be strided: x_stride
+ * elements from a token's row to the next (a multiple of 16 bytes, at least
+ * the row), so that they may be parts of one projection's output. */
+typedef struct {
+    void* pages;
+    void* cold;
+    float* page_sum;
+    int32_t n_layers;
+    int32_t n_pages;
+    int32_t n_cold;
+} hga_pool;
+
+typedef struct {
+    const int32_t* tok_seq;
+    const int32_t* tok_pos;
+    const int32_t* page_table;
+    int32_t n_tokens;
+    int32_t n_seqs;
+    int32_t max_pages;
+} hga_tokens;
+
+/* Bytes of one page in one layer (n_kv_heads * 64 * head_dim * 17/16), or a
+ * negative hga_status.  Host only. */
+int64_t hga_page_bytes(const hga_plan* plan);
+
+/* Chunks a token's list holds at most: keep_first + window + topk_chunks + 1,
+ * window = max(keep_last, force_prev).  Host only. */
+int32_t hga_token_list_size(const hga_plan* plan);
+
+/* Append tokens to the cache: the rows of every token that is not idle and
+ * whose page is present are stored in 4 bits, and every page whose last
+ * position is among them gets its summary.
+ *   k, v  [n_tokens][n_kv_heads][head_dim] plan dtype (strided, see above); K
+ *         rotated at its position
+ * The tokens of one sequence stand next to each other in ascending order of
+ * position (other sequences' before and after), no position twice, and no two
+ * sequences of the call write to one page (hga_copy_pages before appending to
+ * a shared one).  A position may be appended again later (a rejected draft):
+ * pages hold no state besides their rows. */
+hga_status hga_cache_append(const hga_plan* plan, const hga_pool* pool, int32_t layer,
+                            const hga_tokens* tokens, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, void* stream);
+
+/* Read rows back, as hga_gather_kv does from a plain store: the values that
+ * the tokens' stored rows stand for, in the plan's dtype (exactly).
+ *   k_out, v_out  [n_tokens][n_kv_heads][head_dim]; zeros for an idle token or
+ *                 an absent page */
+hga_status hga_cache_read(const hga_plan* plan, const hga_pool* pool, int32_t layer,
+                          const hga_tokens* tokens, void* k_out, void* v_out, void* stream);
+
+/* Bytes hga_route_tokens needs (0 up to 16384 pages), or a negative
+ * hga_status.  Host only. */
+int64_t hga_route_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int32_t max_pages);
+
+/* Route every token by itself (Sec. 3.3 at the grain of a token): with c the
+ * token's own chunk, its list holds chunk c, the visible chunks of
+ * hga_visible_chunks(c) and the topk_chunks middle chunks [keep_first, c -
+ * window) whose summaries have the largest product with the mean of the
+ * token's query heads of the KV head.  Scores are formed in 64 bits; of equal
+ * ones the lowest index is taken; one that is not a number counts as the
+ * lowest.  Absent pages are not listed.
+ *   q           [n_tokens][n_q_heads][head_dim] plan dtype (strided)
+ *   chunk_list  int32 [n_tokens][n_kv_heads][n_list], ascending, padded with
+ *               -1 (all of an idle token's); n_list >= hga_token_list_size
+ *   workspace   hga_route_tokens_workspace bytes, or NULL and 0; calls that
+ *               overlap in time (graphs replayed side by side among them) need
+ *               one each */
+hga_status hga_route_tokens(const hga_plan* plan, const hga_pool* pool, int32_t layer,
+                            const hga_tokens* tokens, const void* q, int64_t q_stride,
+                            int32_t* chunk_list, int32_t n_list, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+
+/* Bytes hga_attend_tokens makes use of at most (n_list 0: every chunk), or a
+ * negative hga_status.  Host only. */
+int64_t hga_attend_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int32_t n_seqs,
+                                    int32_t max_pages, int32_t n_list);
+
+/* Exact softmax attention of every token over the rows, as stored, of the
+ * chunks in its list (or of all its sequence's chunks) at positions up to its
+ * own: scores q.k/sqrt(head_dim), natural-log lse as hga_attend's.  A list
+ * entry that is negative, beyond the token's own chunk or on an absent page
+ * counts for nothing; one that stands twice counts twice.  A token that sees
+ * no row (an idle one among them) gets zeros and an lse of -infinity.
+ *   q, out      [n_tokens][n_q_heads][head_dim] plan dtype (q strided)
+ *   chunk_list  int32 [n_tokens][n_kv_heads][n_list], or NULL with n_list 0
+ *   lse         fp32 [n_tokens][n_q_heads] or NULL
+ *   workspace   any size (hga_attend_tokens_workspace bytes to let long
+ *               histories of few tokens spread over the device), or NULL and
+ *               0; calls that overlap in time need one each.  Its size decides
+ *               the order of the sums, its contents nothing. */
+hga_status hga_attend_tokens(const hga_plan* plan, const hga_pool* pool, int32_t layer,
+                             const hga_tokens* tokens, const void* q, int64_t q_stride,
+                             const int32_t* chunk_list, int32_t n_list, void* out, float* lse,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Copy pages (codes, scales and summary) over others in every layer of the
+ * pool: page src[i] over page dst[i] -- a fork's own copy of a shared page,
+ * pages moved together, pages moved to the cold tier or back.  A pair with an
+ * id outside the pool, or of one id twice, does nothing.  No dst page may stand
+ * among the call's other dst or src pages.
+ *   src, dst  device int32 [n] */
+hga_status hga_copy_pages(const hga_plan* plan, const hga_pool* pool, const int32_t* src,
+                          const int32_t* dst, int32_t n, void* stream);
+
 /* Static description of a status code (never NULL). */
 const char* hga_status_string(int32_t status);
 

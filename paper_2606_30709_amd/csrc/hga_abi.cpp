@@ -10,17 +10,14 @@
 #include <vector>
 
 #include "hga.h"
+#include "abi_common.hpp"
 #include "attend_common.hpp"
 #include "hga_internal.hpp"
 
-namespace {
+namespace hga {
+namespace abi {
 
-// Largest byte extent of one head's slab the kernels address (32-bit
-// offsets, with room above for the "absent" marker offset).
-constexpr int64_t kMaxSlabBytes = 0xfff00000ll;
-
-
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 hga_status fail(hga_status st, const char* fmt, ...) {
     char buf[512];
@@ -37,6 +34,53 @@ hga_status hip_fail(hipError_t e, const char* what) {
 }
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+hga_status check_plan(const hga_plan* plan) {
+    if (!plan) return fail(HGA_EINVAL, "plan is NULL");
+    int dev = -1;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+    if (dev != plan->device)
+        return fail(HGA_EINVAL, "current device %d is not the plan's device %d", dev, plan->device);
+    return HGA_OK;
+}
+
+hga_status check_tensor(const void* p, const char* name) {
+    if (!p) return fail(HGA_EINVAL, "%s is NULL", name);
+    if (!aligned(p, 16)) return fail(HGA_EALIGN, "%s is not 16-byte aligned", name);
+    return HGA_OK;
+}
+
+hga_status check_workspace(const void* workspace, int64_t workspace_bytes) {
+    if (workspace_bytes < 0) return fail(HGA_EINVAL, "workspace_bytes must be >= 0");
+    if (workspace_bytes > 0) {
+        if (!workspace) return fail(HGA_EINVAL, "workspace is NULL with workspace_bytes > 0");
+        if (!aligned(workspace, 16)) return fail(HGA_EALIGN, "workspace is not 16-byte aligned");
+    }
+    return HGA_OK;
+}
+
+hga_status check_index(const void* p, const char* name) {
+    if (!p) return fail(HGA_EINVAL, "%s is NULL", name);
+    if (!aligned(p, 4)) return fail(HGA_EALIGN, "%s is not 4-byte aligned", name);
+    return HGA_OK;
+}
+
+hga_status launched(hipError_t e, const char* what) {
+    if (e != hipSuccess) return hip_fail(e, what);
+    return HGA_OK;
+}
+
+}  // namespace abi
+}  // namespace hga
+
+using namespace hga::abi;
+
+namespace {
+
+// Largest byte extent of one head's slab the kernels address (32-bit
+// offsets, with room above for the "absent" marker offset).
+constexpr int64_t kMaxSlabBytes = 0xfff00000ll;
 
 // Pair p is high-frequency for a span when its wavelength 2*pi/theta_p is at
 // most the span (Sec. 3.2 leaves the split open; this is the rule used).
@@ -115,56 +159,8 @@ hga_status validate_params(const hga_params* p) {
     return HGA_OK;
 }
 
-hga_status check_plan(const hga_plan* plan) {
-    if (!plan) return fail(HGA_EINVAL, "plan is NULL");
-    int dev = -1;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
-    if (dev != plan->device)
-        return fail(HGA_EINVAL, "current device %d is not the plan's device %d", dev, plan->device);
-    return HGA_OK;
-}
-
-hga_status check_tensor(const void* p, const char* name) {
-    if (!p) return fail(HGA_EINVAL, "%s is NULL", name);
-    if (!aligned(p, 16)) return fail(HGA_EALIGN, "%s is not 16-byte aligned", name);
-    return HGA_OK;
-}
-
 // Most slots a warm-cache partition may have (its LRU keys live in LDS).
 constexpr int32_t kMaxCacheSlots = 8192;
-
-// A caller workspace: NULL with 0 bytes, or 16-byte aligned with > 0 bytes.
-hga_status check_workspace(const void* workspace, int64_t workspace_bytes) {
-    if (workspace_bytes < 0) return fail(HGA_EINVAL, "workspace_bytes must be >= 0");
-    if (workspace_bytes > 0) {
-        if (!workspace) return fail(HGA_EINVAL, "workspace is NULL with workspace_bytes > 0");
-        if (!aligned(workspace, 16)) return fail(HGA_EALIGN, "workspace is not 16-byte aligned");
-    }
-    return HGA_OK;
-}
-
-hga_status check_index(const void* p, const char* name) {
-    if (!p) return fail(HGA_EINVAL, "%s is NULL", name);
-    if (!aligned(p, 4)) return fail(HGA_EALIGN, "%s is not 4-byte aligned", name);
-    return HGA_OK;
-}
-
-hga_status launched(hipError_t e, const char* what) {
-    if (e != hipSuccess) return hip_fail(e, what);
-    return HGA_OK;
-}
-
-// A launch reports its error through hipGetLastError(), which also returns
-// errors that earlier, unrelated runtime calls on this thread left behind;
-// clear those first so a launch is charged only with its own failure.
-void clear_stale_error() { (void)hipGetLastError(); }
-
-#define HGA_TRY(x)                      \
-    do {                                \
-        hga_status st_ = (x);           \
-        if (st_ != HGA_OK) return st_;  \
-    } while (0)
 
 }  // namespace
 
@@ -194,7 +190,7 @@ const char* hga_status_string(int32_t status) {
     }
 }
 
-const char* hga_last_error(void) { return g_last_error.c_str(); }
+const char* hga_last_error(void) { return hga::abi::g_last_error.c_str(); }
 
 hga_status hga_plan_create(const hga_params* params, hga_plan** plan) {
     if (!plan) return fail(HGA_EINVAL, "plan out-pointer is NULL");

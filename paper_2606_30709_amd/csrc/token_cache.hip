@@ -1,0 +1,270 @@
+// The paged 4-bit cache: appending tokens, reading rows back, copying pages.
+//
+// Append and read move a row of a head with D/8 lanes, eight dimensions each: the four lanes of a 32-dimension block find
+// the block's largest magnitude among themselves, and a lane's eight codes are one word of the page.  Both are bound by
+// their bytes (a token of 4 heads of d128: 2 KiB of bf16 in, 544 bytes out).
+#include "hga_device.hpp"
+#include "hga_internal.hpp"
+#include "tokens.hpp"
+
+namespace hga {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Largest of the four lanes of a quad.
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
+    uint32_t o = static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0xB1, 0xf, 0xf, true));
+    x = o > x ? o : x;
+    o = static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x4E, 0xf, 0xf, true));
+    return o > x ? o : x;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void append_kernel(PoolView pool, TokensView tok, const T* __restrict__ k,
+                                                          int64_t k_stride, const T* __restrict__ v,
+                                                          int64_t v_stride) {
+    using F = PageFormat<D>;
+    constexpr int kLanes = 2 * D / 8;  // lanes of a (token, head): keys, then values
+    const int64_t item = static_cast<int64_t>(linear_block<kThreads>()) * (kThreads / kLanes) + threadIdx.x / kLanes;
+    const int t = static_cast<int>(item / pool.n_kv), h = static_cast<int>(item % pool.n_kv);
+    if (t >= tok.n_tokens) return;
+    int s, p;
+    if (!tok.at(t, s, p)) return;
+    const int id = tok.page_id(s, p / kPageRows);
+    if (!pool.has(id)) return;
+    const int lane = threadIdx.x % kLanes;
+    const bool key = lane < D / 8;
+    const int dim = lane % (D / 8) * 8, row = p % kPageRows;
+    float x[8];
+    load8((key ? k + t * k_stride : v + t * v_stride) + h * D + dim, x);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    const uint32_t e = block_scale(quad_max(m));
+    const uint32_t codes = encode8(x, e);
+    unsigned char* head = pool.page(id) + h * F::kBytes;
+    if (key) {
+        *reinterpret_cast<uint32_t*>(head + F::key_code(row, dim)) = codes;
+        if (dim % 32 == 0) head[F::key_scale(row, dim / 32)] = static_cast<unsigned char>(e);
+    } else {
+        if constexpr (F::kLaneDims == 8) {
+            *reinterpret_cast<uint32_t*>(head + F::value_code(row, dim)) = codes;
+        } else {
+            *reinterpret_cast<uint16_t*>(head + F::value_code(row, dim)) = static_cast<uint16_t>(codes);
+            *reinterpret_cast<uint16_t*>(head + F::value_code(row, dim + 4)) = static_cast<uint16_t>(codes >> 16);
+        }
+        if (dim % 32 == 0) head[F::value_scale(row, dim / 32)] = static_cast<unsigned char>(e);
+    }
+}
+
+// Summary of every page that a token of the call fills (the token at its last row): the mean over the page's stored keys
+// turned to the page's middle, as the chunk summaries'.  A wavefront per (token, head).
+template <int D>
+__global__ __launch_bounds__(kThreads) void close_kernel(PoolView pool, TokensView tok,
+                                                         const float* __restrict__ phase_group,
+                                                         const float* __restrict__ phase_psi, int group, int hf_chunk) {
+    using F = PageFormat<D>;
+    constexpr int HALF = D / 2;
+    const int64_t item = static_cast<int64_t>(linear_block<kThreads>()) * (kThreads / 64) + threadIdx.x / 64;
+    const int t = static_cast<int>(item / pool.n_kv), h = static_cast<int>(item % pool.n_kv);
+    if (t >= tok.n_tokens) return;
+    int s, p;
+    if (!tok.at(t, s, p) || p % kPageRows != kPageRows - 1) return;
+    const int id = tok.page_id(s, p / kPageRows);
+    if (!pool.has(id)) return;
+    const unsigned char* head = pool.page(id) + h * F::kBytes;
+    const int lane = threadIdx.x & 63;
+    const int pair = lane % HALF;
+    if (lane >= HALF) return;
+    const int gpc = kPageRows / group;
+    const bool turn = pair >= hf_chunk;
+    float sa = 0.f, sb = 0.f;
+    for (int g = 0; g < gpc; ++g) {
+        float ga = 0.f, gb = 0.f;
+        for (int o = 0; o < group; ++o) {
+            const int row = g * group + o;
+            const int shift = 4 * (pair & 1);
+            auto value = [&](int dim) {
+                const uint32_t code = head[F::key_code(row, dim)] >> shift & 15u;
+                return __uint_as_float(decode2<0>(code, scale_of(head[F::key_scale(row, dim / 32)])) << 16);
+            };
+            const float a = value(pair), b = value(pair + HALF);
+            const float c = turn ? phase_group[o * HALF + pair] : 1.f;
+            const float sn = turn ? phase_group[(group + o) * HALF + pair] : 0.f;
+            ga += a * c - b * sn;
+            gb += a * sn + b * c;
+        }
+        const float c = turn ? phase_psi[g * HALF + pair] : 1.f;
+        const float sn = turn ? phase_psi[(gpc + g) * HALF + pair] : 0.f;
+        sa += ga * c - gb * sn;
+        sb += ga * sn + gb * c;
+    }
+    float* out = pool.sum + (static_cast<int64_t>(id) * pool.n_kv + h) * D;
+    out[pair] = sa * (1.f / kPageRows);
+    out[pair + HALF] = sb * (1.f / kPageRows);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void read_kernel(PoolView pool, TokensView tok, T* __restrict__ k,
+                                                        T* __restrict__ v) {
+    using F = PageFormat<D>;
+    constexpr int kLanes = 2 * D / 8;
+    const int64_t item = static_cast<int64_t>(linear_block<kThreads>()) * (kThreads / kLanes) + threadIdx.x / kLanes;
+    const int t = static_cast<int>(item / pool.n_kv), h = static_cast<int>(item % pool.n_kv);
+    if (t >= tok.n_tokens) return;
+    const int lane = threadIdx.x % kLanes;
+    const bool key = lane < D / 8;
+    const int dim = lane % (D / 8) * 8;
+    int s, p;
+    const bool in = tok.at(t, s, p);
+    const int id = in ? tok.page_id(s, p / kPageRows) : -1;
+    uint32_t codes = 0;
+    uint32_t e = 127;
+    if (in && pool.has(id)) {
+        const int row = p % kPageRows;
+        const unsigned char* head = pool.page(id) + h * F::kBytes;
+        if (key) {
+            codes = *reinterpret_cast<const uint32_t*>(head + F::key_code(row, dim));
+        } else if constexpr (F::kLaneDims == 8) {
+            codes = *reinterpret_cast<const uint32_t*>(head + F::value_code(row, dim));
+        } else {
+            codes = *reinterpret_cast<const uint16_t*>(head + F::value_code(row, dim)) |
+                    static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(head + F::value_code(row, dim + 4))) << 16;
+        }
+        e = head[key ? F::key_scale(row, dim / 32) : F::value_scale(row, dim / 32)];
+    }
+    const float sc = scale_of(e);
+    vec16 b;
+    b.w[0] = decode2<0>(codes, sc);
+    b.w[1] = decode2<1>(codes, sc);
+    b.w[2] = decode2<2>(codes, sc);
+    b.w[3] = decode2<3>(codes, sc);
+    T* out = (key ? k : v) + item * D + dim;
+    if constexpr (sizeof(T) == 2) {
+        store16(out, b);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            vec16 w;
+            w.w[0] = b.w[2 * i] << 16;
+            w.w[1] = b.w[2 * i] & 0xffff0000u;
+            w.w[2] = b.w[2 * i + 1] << 16;
+            w.w[3] = b.w[2 * i + 1] & 0xffff0000u;
+            store16(out + 4 * i, w);
+        }
+    }
+}
+
+// Copies page src[i] over page dst[i] in every layer, summaries too.  A workgroup takes kCopyBytes of one pair's page (or
+// its summary) in one layer.
+constexpr int kCopyBytes = kThreads * 16 * 4;
+
+struct CopyArgs {
+    unsigned char *hot, *cold;
+    float* sum;
+    int n_hot, n_cold, n_layers;
+    int64_t page_bytes, sum_bytes;  // of one page in one layer
+    int slices, sum_slices;         // workgroups of a page's bytes, of its summary's
+};
+
+__global__ __launch_bounds__(kThreads) void copy_kernel(CopyArgs a, const int32_t* __restrict__ src,
+                                                        const int32_t* __restrict__ dst, int n) {
+    const int64_t block = linear_block<kThreads>();
+    const int per = a.slices + a.sum_slices;
+    const int slice = static_cast<int>(block % per);
+    const int64_t pl = block / per;
+    const int layer = static_cast<int>(pl / n), i = static_cast<int>(pl % n);
+    if (layer >= a.n_layers) return;
+    const int from = src[i], to = dst[i];
+    const uint32_t ids = static_cast<uint32_t>(a.n_hot) + static_cast<uint32_t>(a.n_cold);
+    if (static_cast<uint32_t>(from) >= ids || static_cast<uint32_t>(to) >= ids || from == to) return;
+    const bool page = slice < a.slices;
+    auto at = [&](int id) -> unsigned char* {
+        if (!page) return reinterpret_cast<unsigned char*>(a.sum) + (static_cast<int64_t>(layer) * ids + id) * a.sum_bytes;
+        return id < a.n_hot ? a.hot + (static_cast<int64_t>(layer) * a.n_hot + id) * a.page_bytes
+                            : a.cold + (static_cast<int64_t>(layer) * a.n_cold + id - a.n_hot) * a.page_bytes;
+    };
+    const int64_t bytes = page ? a.page_bytes : a.sum_bytes;
+    const int64_t b0 = static_cast<int64_t>(page ? slice : slice - a.slices) * kCopyBytes + threadIdx.x * 16;
+    const unsigned char* f = at(from);
+    unsigned char* d = at(to);
+    vec16 x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (b0 + j * kThreads * 16 < bytes) x[j] = load16(f + b0 + j * kThreads * 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (b0 + j * kThreads * 16 < bytes) store16(d + b0 + j * kThreads * 16, x[j]);
+}
+
+int64_t items(const hga_plan& plan, const TokensView& tok) {
+    return static_cast<int64_t>(tok.n_tokens) * plan.p.n_kv_heads;
+}
+
+template <typename T, int D>
+hipError_t append_t(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const void* k, int64_t k_stride,
+                    const void* v, int64_t v_stride, hipStream_t stream) {
+    constexpr int per = kThreads / (2 * D / 8);
+    const int64_t n = items(plan, tok);
+    append_kernel<T, D><<<grid_of((n + per - 1) / per, kThreads), kThreads, 0, stream>>>(
+        pool, tok, static_cast<const T*>(k), k_stride, static_cast<const T*>(v), v_stride);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    close_kernel<D><<<grid_of((n + 3) / 4, kThreads), kThreads, 0, stream>>>(pool, tok, plan.phase_group, plan.phase_psi,
+                                                                            plan.p.group, plan.p.hf_pairs_chunk);
+    return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t read_t(const hga_plan& plan, const PoolView& pool, const TokensView& tok, void* k, void* v,
+                  hipStream_t stream) {
+    constexpr int per = kThreads / (2 * D / 8);
+    read_kernel<T, D><<<grid_of((items(plan, tok) + per - 1) / per, kThreads), kThreads, 0, stream>>>(
+        pool, tok, static_cast<T*>(k), static_cast<T*>(v));
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache_append(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, hipStream_t stream) {
+    const bool f32 = plan.p.dtype == HGA_F32;
+    const auto f = plan.p.head_dim == 128 ? (f32 ? append_t<float, 128> : append_t<bf16_t, 128>)
+                                          : (f32 ? append_t<float, 64> : append_t<bf16_t, 64>);
+    return f(plan, pool, tok, k, k_stride, v, v_stride, stream);
+}
+
+hipError_t launch_cache_read(const hga_plan& plan, const PoolView& pool, const TokensView& tok, void* k, void* v,
+                             hipStream_t stream) {
+    const bool f32 = plan.p.dtype == HGA_F32;
+    const auto f = plan.p.head_dim == 128 ? (f32 ? read_t<float, 128> : read_t<bf16_t, 128>)
+                                          : (f32 ? read_t<float, 64> : read_t<bf16_t, 64>);
+    return f(plan, pool, tok, k, v, stream);
+}
+
+int64_t copy_pages_workgroups(const hga_plan& plan) {
+    const int64_t page = static_cast<int64_t>(plan.p.n_kv_heads) * page_head_bytes(plan.p.head_dim);
+    const int64_t sum = static_cast<int64_t>(plan.p.n_kv_heads) * plan.p.head_dim * 4;
+    return (page + kCopyBytes - 1) / kCopyBytes + (sum + kCopyBytes - 1) / kCopyBytes;
+}
+
+hipError_t launch_copy_pages(const hga_plan& plan, const hga_pool& pool, void* cold, const int32_t* src,
+                             const int32_t* dst, int n, hipStream_t stream) {
+    CopyArgs a;
+    a.hot = static_cast<unsigned char*>(pool.pages);
+    a.cold = static_cast<unsigned char*>(cold);
+    a.sum = pool.page_sum;
+    a.n_hot = pool.n_pages;
+    a.n_cold = pool.n_cold;
+    a.n_layers = pool.n_layers;
+    a.page_bytes = static_cast<int64_t>(plan.p.n_kv_heads) * page_head_bytes(plan.p.head_dim);
+    a.sum_bytes = static_cast<int64_t>(plan.p.n_kv_heads) * plan.p.head_dim * 4;
+    a.slices = static_cast<int>((a.page_bytes + kCopyBytes - 1) / kCopyBytes);
+    a.sum_slices = static_cast<int>((a.sum_bytes + kCopyBytes - 1) / kCopyBytes);
+    const int64_t blocks = static_cast<int64_t>(n) * a.n_layers * (a.slices + a.sum_slices);
+    copy_kernel<<<grid_of(blocks, kThreads), kThreads, 0, stream>>>(a, src, dst, n);
+    return hipGetLastError();
+}
+
+}  // namespace hga

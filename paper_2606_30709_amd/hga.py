@@ -23,6 +23,9 @@ __all__ = [
     "hga_gather_attend_split", "hga_gather_kv_cached", "hga_attend_backward",
     "hga_attend_backward_write", "hga_block_step", "hga_prefill_blocks", "hga_status_string", "hga_last_error",
     "hga_version", "hga_visible_chunks", "EXPORTED_SYMBOLS",
+    "Pool", "TokenBatch", "hga_page_bytes", "hga_token_list_size", "hga_cache_append",
+    "hga_cache_read", "hga_route_tokens", "hga_route_tokens_workspace", "hga_attend_tokens",
+    "hga_attend_tokens_workspace", "hga_copy_pages",
 ]
 
 F32, BF16 = 0, 1
@@ -37,6 +40,9 @@ EXPORTED_SYMBOLS = (
     "hga_gather_kv_cached", "hga_attend_backward", "hga_attend_backward_write",
     "hga_block_step", "hga_prefill_blocks", "hga_status_string",
     "hga_last_error", "hga_version", "hga_visible_chunks",
+    "hga_page_bytes", "hga_token_list_size", "hga_cache_append", "hga_cache_read",
+    "hga_route_tokens", "hga_route_tokens_workspace", "hga_attend_tokens",
+    "hga_attend_tokens_workspace", "hga_copy_pages",
 )
 
 
@@ -56,6 +62,21 @@ class HgaParams(ctypes.Structure):
         ("topk_groups", ctypes.c_int32), ("hf_pairs_chunk", ctypes.c_int32),
         ("hf_pairs_group", ctypes.c_int32), ("dtype", ctypes.c_int32),
         ("rope_base", ctypes.c_double),
+    ]
+
+
+class HgaPool(ctypes.Structure):
+    _fields_ = [
+        ("pages", ctypes.c_void_p), ("cold", ctypes.c_void_p), ("page_sum", ctypes.c_void_p),
+        ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_cold", ctypes.c_int32),
+    ]
+
+
+class HgaTokens(ctypes.Structure):
+    _fields_ = [
+        ("tok_seq", ctypes.c_void_p), ("tok_pos", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p), ("n_tokens", ctypes.c_int32),
+        ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32),
     ]
 
 
@@ -111,6 +132,23 @@ def library() -> ctypes.CDLL:
             fn = getattr(lib, name)
             fn.argtypes = args
             fn.restype = i32
+        pool_p, tok_p = ctypes.POINTER(HgaPool), ctypes.POINTER(HgaTokens)
+        more = {
+            "hga_page_bytes": ([vp], i64),
+            "hga_token_list_size": ([vp], i32),
+            "hga_cache_append": ([vp, pool_p, i32, tok_p, vp, i64, vp, i64, vp], i32),
+            "hga_cache_read": ([vp, pool_p, i32, tok_p, vp, vp, vp], i32),
+            "hga_route_tokens_workspace": ([vp, i32, i32], i64),
+            "hga_route_tokens": ([vp, pool_p, i32, tok_p, vp, i64, vp, i32, vp, i64, vp], i32),
+            "hga_attend_tokens_workspace": ([vp, i32, i32, i32, i32], i64),
+            "hga_attend_tokens": ([vp, pool_p, i32, tok_p, vp, i64, vp, i32, vp, vp, vp, i64, vp],
+                                  i32),
+            "hga_copy_pages": ([vp, pool_p, vp, vp, i32, vp], i32),
+        }
+        for name, (args, res) in more.items():
+            fn = getattr(lib, name)
+            fn.argtypes = args
+            fn.restype = res
         lib.hga_attend_split_workspace.argtypes = [vp, i32]
         lib.hga_attend_split_workspace.restype = i64
         lib.hga_static_scratch_bytes.argtypes = []
@@ -465,3 +503,199 @@ def hga_prefill_blocks(plan: Plan, q_blocks, k_res, v_res, chunk_sum, group_sum,
         _ptr(chunk_sum), _ptr(group_sum), chunk_sum.shape[2], _ptr(qbar), _ptr(chunk_idx),
         _ptr(group_idx), _ptr(k_routed), _ptr(v_routed), _ptr(out), _ptr(lse), *_ws(workspace),
         _stream(stream)))
+
+
+# ------------------------------------- single tokens over a paged 4-bit cache ---
+
+def _require(ok, message: str):
+    if not ok:
+        raise HgaError(-1, f"HGA_EINVAL: {message}")
+
+
+def _expect(t, name: str, dtype, shape, device=None, contiguous=True):
+    """A tensor argument as the call takes it (None in shape: any size)."""
+    _require(isinstance(t, torch.Tensor), f"{name} must be a tensor")
+    _require(t.dtype == dtype, f"{name} must be {dtype}, is {t.dtype}")
+    _require(t.dim() == len(shape) and all(w is None or w == n for n, w in zip(t.shape, shape)),
+             f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
+    _require(not contiguous or t.is_contiguous(), f"{name} must be contiguous")
+    if device is not None:
+        _require(t.device == device, f"{name} must be on {device}, is on {t.device}")
+
+
+def _rows(t, name: str, plan: Plan, n_tokens: int, heads: int, device) -> int:
+    """Elements from a token's row to the next of t [n_tokens, heads, head_dim]."""
+    d = plan.params.head_dim
+    _expect(t, name, plan.torch_dtype, (n_tokens, heads, d), device, contiguous=False)
+    _require(n_tokens == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d)),
+             f"{name}: a token's heads must be contiguous")
+    # a single token's stride means nothing (and may be anything)
+    return t.stride(0) if n_tokens > 1 else heads * d
+
+
+class Pool:
+    """Buffers of a paged 4-bit cache: ``pages`` uint8 [n_layers, n_pages,
+    n_kv_heads, bytes], ``page_sum`` fp32 [n_layers, n_pages + n_cold,
+    n_kv_heads, head_dim] and, with ``n_cold`` pages of a cold tier, ``cold``
+    (as pages, pinned host memory).  Given tensors are used as they are."""
+
+    def __init__(self, plan: Plan, n_pages: int | None = None, n_layers: int = 1, n_cold: int = 0,
+                 device="cuda", pages=None, page_sum=None, cold=None):
+        p = plan.params
+        head = hga_page_bytes(plan) // p.n_kv_heads
+        if pages is None:
+            _require(n_pages is not None and n_pages >= 0, "n_pages must be >= 0")
+            pages = torch.zeros(n_layers, n_pages, p.n_kv_heads, head, dtype=torch.uint8,
+                                device=device)
+        _expect(pages, "pages", torch.uint8, (None, None, p.n_kv_heads, head))
+        _require(pages.is_cuda, "pages must be on a GPU")
+        n_layers, n_pages = pages.shape[:2]
+        if cold is None and n_cold:
+            cold = torch.zeros(n_layers, n_cold, p.n_kv_heads, head, dtype=torch.uint8,
+                               pin_memory=True)
+        if cold is not None:
+            _expect(cold, "cold", torch.uint8, (n_layers, None, p.n_kv_heads, head))
+            _require(cold.is_pinned(), "cold must be pinned host memory")
+            n_cold = cold.shape[1]
+        if page_sum is None:
+            page_sum = torch.zeros(n_layers, n_pages + n_cold, p.n_kv_heads, p.head_dim,
+                                   device=pages.device)
+        _expect(page_sum, "page_sum", torch.float32,
+                (n_layers, n_pages + n_cold, p.n_kv_heads, p.head_dim), pages.device)
+        self.pages, self.page_sum, self.cold = pages, page_sum, cold
+        self.n_layers, self.n_pages, self.n_cold = n_layers, n_pages, n_cold
+        self.device = pages.device
+        self.struct = HgaPool(pages.data_ptr(), None if cold is None else cold.data_ptr(),
+                              page_sum.data_ptr(), n_layers, n_pages, n_cold)
+
+
+class TokenBatch:
+    """The tokens of a call: token t is position ``tok_pos[t]`` of sequence
+    ``tok_seq[t]`` (int32 [n_tokens]), whose chunk c lies in page
+    ``page_table[tok_seq[t], c]`` (int32 [n_seqs, max_pages]).  The tensors are
+    used in place: their contents may change between calls."""
+
+    def __init__(self, tok_seq, tok_pos, page_table):
+        dev = page_table.device
+        _expect(page_table, "page_table", torch.int32, (None, None), dev)
+        _expect(tok_seq, "tok_seq", torch.int32, (None,), dev)
+        _expect(tok_pos, "tok_pos", torch.int32, (tok_seq.shape[0],), dev)
+        _require(page_table.is_cuda, "page_table must be on a GPU")
+        self.tok_seq, self.tok_pos, self.page_table = tok_seq, tok_pos, page_table
+        self.n_tokens = tok_seq.shape[0]
+        self.n_seqs, self.max_pages = page_table.shape
+        self.device = dev
+        self.struct = HgaTokens(tok_seq.data_ptr(), tok_pos.data_ptr(), page_table.data_ptr(),
+                                self.n_tokens, self.n_seqs, self.max_pages)
+
+
+def _size(n: int) -> int:
+    if n < 0:
+        _check(n)
+    return n
+
+
+def _same_device(pool: Pool, batch: TokenBatch):
+    _require(pool.device == batch.device,
+             f"the batch is on {batch.device}, the pool on {pool.device}")
+    _on_current(pool)
+
+
+def _on_current(pool: Pool):
+    _require(pool.device.index == torch.cuda.current_device(),
+             f"the pool is on {pool.device}, the current device is {torch.cuda.current_device()}")
+
+
+def hga_page_bytes(plan: Plan) -> int:
+    """Bytes of one page in one layer."""
+    return _size(library().hga_page_bytes(plan.handle))
+
+
+def hga_token_list_size(plan: Plan) -> int:
+    """Chunks hga_route_tokens lists for a token at most."""
+    return _size(library().hga_token_list_size(plan.handle))
+
+
+def hga_cache_append(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, k, v, stream=None):
+    """Stores k, v [n_tokens, n_kv_heads, head_dim] (token rows may be strided)
+    in the tokens' pages in 4 bits and summarises the pages they fill."""
+    _same_device(pool, batch)
+    kv, dev = plan.params.n_kv_heads, pool.device
+    ks = _rows(k, "k", plan, batch.n_tokens, kv, dev)
+    vs = _rows(v, "v", plan, batch.n_tokens, kv, dev)
+    _check(library().hga_cache_append(
+        plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct), _ptr(k), ks,
+        _ptr(v), vs, _stream(stream)))
+
+
+def hga_cache_read(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, k_out, v_out,
+                   stream=None):
+    """The values that the tokens' stored rows stand for, into k_out, v_out
+    [n_tokens, n_kv_heads, head_dim]."""
+    _same_device(pool, batch)
+    shape = (batch.n_tokens, plan.params.n_kv_heads, plan.params.head_dim)
+    _expect(k_out, "k_out", plan.torch_dtype, shape, pool.device)
+    _expect(v_out, "v_out", plan.torch_dtype, shape, pool.device)
+    _check(library().hga_cache_read(
+        plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct), _ptr(k_out),
+        _ptr(v_out), _stream(stream)))
+
+
+def hga_route_tokens_workspace(plan: Plan, batch: TokenBatch) -> int:
+    """Bytes of workspace hga_route_tokens needs for the batch (often 0)."""
+    return _size(library().hga_route_tokens_workspace(plan.handle, batch.n_tokens,
+                                                      batch.max_pages))
+
+
+def hga_route_tokens(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, q, chunk_list,
+                     workspace=None, stream=None):
+    """Each token's chunks into chunk_list int32 [n_tokens, n_kv_heads, n_list]
+    (ascending, -1 behind); q [n_tokens, n_q_heads, head_dim], rows may be
+    strided."""
+    _same_device(pool, batch)
+    qs = _rows(q, "q", plan, batch.n_tokens, plan.params.n_q_heads, pool.device)
+    _expect(chunk_list, "chunk_list", torch.int32,
+            (batch.n_tokens, plan.params.n_kv_heads, None), pool.device)
+    _check(library().hga_route_tokens(
+        plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct), _ptr(q), qs,
+        _ptr(chunk_list), chunk_list.shape[2], *_ws(workspace), _stream(stream)))
+
+
+def hga_attend_tokens_workspace(plan: Plan, batch: TokenBatch, chunk_list=None) -> int:
+    """Bytes of workspace hga_attend_tokens makes use of at most."""
+    n_list = 0 if chunk_list is None else chunk_list.shape[2]
+    return _size(library().hga_attend_tokens_workspace(
+        plan.handle, batch.n_tokens, batch.n_seqs, batch.max_pages, n_list))
+
+
+def hga_attend_tokens(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, q, out, lse=None,
+                      chunk_list=None, workspace=None, stream=None):
+    """Attention of each token over the chunks in its list (None: all of its
+    sequence's) up to its own position.  q, out [n_tokens, n_q_heads, head_dim]
+    (q's rows may be strided); lse fp32 [n_tokens, n_q_heads] or None;
+    workspace: a device tensor, or None."""
+    _same_device(pool, batch)
+    p = plan.params
+    qs = _rows(q, "q", plan, batch.n_tokens, p.n_q_heads, pool.device)
+    _expect(out, "out", plan.torch_dtype, (batch.n_tokens, p.n_q_heads, p.head_dim), pool.device)
+    if lse is not None:
+        _expect(lse, "lse", torch.float32, (batch.n_tokens, p.n_q_heads), pool.device)
+    n_list = 0
+    if chunk_list is not None:
+        _expect(chunk_list, "chunk_list", torch.int32, (batch.n_tokens, p.n_kv_heads, None),
+                pool.device)
+        n_list = chunk_list.shape[2]
+        _require(n_list > 0, "chunk_list must hold an entry a token")
+    _check(library().hga_attend_tokens(
+        plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct), _ptr(q), qs,
+        _ptr(chunk_list), n_list, _ptr(out), _ptr(lse), *_ws(workspace), _stream(stream)))
+
+
+def hga_copy_pages(plan: Plan, pool: Pool, src, dst, stream=None):
+    """Copies page src[i] over page dst[i] (int32 [n], on the GPU) in every
+    layer, summaries included."""
+    _on_current(pool)
+    _expect(src, "src", torch.int32, (None,), pool.device)
+    _expect(dst, "dst", torch.int32, (src.shape[0],), pool.device)
+    _check(library().hga_copy_pages(plan.handle, ctypes.byref(pool.struct), _ptr(src), _ptr(dst),
+                                    src.shape[0], _stream(stream)))
