@@ -1,25 +1,30 @@
 // Attention of single tokens over the paged 4-bit cache (Sec. 3.4 at the token's grain, every query head of a KV head in
 // one tile).
 //
-// A unit is (token, KV head).  Its query heads are the columns of a 16-column tile:
-//   S^T [16 keys x 16 heads] = K~ [16 x d] q^T      (d/32 instructions of 16x16x32)
-//   O^T [16 dims x 16 heads] += V~^T [16 x 32] P^T  (a 32-key half page, d/16 instructions)
+// A unit is one KV head and one token, or (over whole histories) up to 16 kTiles / r adjacent tokens of one sequence: its
+// query heads are the columns of kTiles 16-column tiles,
+//   S^T [16 keys x 16 columns] = K~ [16 x d] q^T      (d/32 instructions of 16x16x32)
+//   O^T [16 dims x 16 columns] += V~^T [16 x 32] P^T  (a 32-key half page, d/16 instructions)
 // Codes become bf16 in registers, two an instruction with their scale.  The layout of a page (tokens.hpp) is that of these
 // operands, so codes go straight from memory to the lane that multiplies them.  A lane of S^T holds keys 4 g .. 4 g + 3 of
 // its tile, and takes those as its reduction indices of the second product: P never leaves the lane.  One pass over the
-// keys with the running maximum and sum (in log2 units) of each head.
+// keys with a running reference (the maximum, or up to 2^kSlack below it) and sum of each column, in log2 units.
 //
 // fp32 queries and weights enter the matrix instructions as three bf16 terms each (24 bits); the stored keys and values are
 // exact in bf16.
+//
+// A wavefront loads its next page while it works on one; the wavefronts of a workgroup take every kWaves-th page and are
+// joined in LDS.  Long histories of few units are cut into equal runs of pages, a workgroup each, whose partial results a
+// second kernel joins in order.
+#include <algorithm>
+#include <type_traits>
+
 #include "hga_device.hpp"
 #include "hga_internal.hpp"
 #include "tokens.hpp"
 
 namespace hga {
 namespace {
-
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -48,264 +53,582 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t* w) {
     }
 }
 
+// A lane's share of a page's keys and of its values.
 template <int D>
-struct Page {  // a lane's share of a page
-    uint32_t k[4][D / 32];
-    uint32_t v[4][D / 32];
-    uint32_t ks;
-    uint32_t vs[4];
+struct Keys {
+    uint32_t c[4][D / 32];
+    uint32_t s;
+};
+template <int D>
+struct Values {
+    uint32_t c[4][D / 32];
+    uint32_t s[4];
 };
 
+// One head's part of a page as a buffer: no address arithmetic per lane but a fixed offset, and an empty buffer's loads
+// touch no memory, so that the loop below needs no branch around its last loads.
 template <int D>
-__device__ __forceinline__ void load_codes(const unsigned char* p, uint32_t* w) {
+__device__ __forceinline__ void load_codes(buf_rsrc r, uint32_t offset, uint32_t (&w)[D / 32]) {
     if constexpr (D == 128) {
-        const vec16 x = load16(p);
+        const vec16 x = buf_load16(r, offset);
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = x.w[i];
     } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 0));
         w[0] = x.x;
         w[1] = x.y;
     }
 }
-
 template <int D>
-__device__ __forceinline__ void load_page(const unsigned char* head, int m, int g, Page<D>& pg) {
+__device__ __forceinline__ void load_keys(buf_rsrc r, int m, int g, Keys<D>& k) {
     using F = PageFormat<D>;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) load_codes<D>(head + F::key_code(16 * t + m, g * (D / 4)), pg.k[t]);
-    pg.ks = *reinterpret_cast<const uint32_t*>(head + F::key_scale(m, g * (D / 4) / 32));
+    for (int t = 0; t < 4; ++t) load_codes<D>(r, F::key_code(m, g * (D / 4)) + t * F::key_code(16, 0), k.c[t]);
+    k.s = static_cast<uint32_t>(buf_load_i32(r, F::key_scale(m, g * (D / 4) / 32)));
+}
+template <int D>
+__device__ __forceinline__ void load_values(buf_rsrc r, int m, int g, Values<D>& v) {
+    using F = PageFormat<D>;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) load_codes<D>(head + F::value_code(16 * t + 4 * g, m * F::kLaneDims), pg.v[t]);
-    const vec16 x = load16(head + F::value_scale(4 * g, m * F::kLaneDims / 32));
+    for (int t = 0; t < 4; ++t)
+        load_codes<D>(r, F::value_code(4 * g, m * F::kLaneDims) + t * (F::value_code(16, 0) - F::kCodes), v.c[t]);
+    const vec16 x = buf_load16(r, F::value_scale(4 * g, m * F::kLaneDims / 32));
 #pragma unroll
-    for (int t = 0; t < 4; ++t) pg.vs[t] = x.w[t];
+    for (int t = 0; t < 4; ++t) v.s[t] = x.w[t];
 }
 
+// The maximum (sum) of the four lanes that share a column, in all of them.
 __device__ __forceinline__ float max_groups(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const uint32_t v = __float_as_uint(x);
+    const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float sum_groups(float x) {
     x += __shfl_xor(x, 16);
     return x + __shfl_xor(x, 32);
 }
 
+// A reference below the maximum by this (log2) stays: weights reach 2^kSlack, exact in fp32 and within bf16's range.
+constexpr float kSlack = 8.0f;
+
 struct AttendArgs {
     const int32_t* list;  // NULL: every chunk
     int n_list, ratio;
+    int run;              // pages of a workgroup
+    int splits;           // workgroups of a unit at most
     float* lse;
+    const int32_t* units;  // [0]: how many, then their first tokens and the call's end; NULL: every token is a unit
+    int32_t* parts;       // [token]: workgroups that took its unit
+    float* part;          // their results [split][token][query head][d], not divided by the sum
+    float* part_ml;       // ... and [split][token][query head][2]: reference, sum
 };
 
-// A workgroup per unit; its wavefronts take every fourth page each and are joined in LDS.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void attend_tokens_kernel(PoolView pool, TokensView tok, AttendArgs a,
-                                                                 const T* __restrict__ q, int64_t q_stride,
-                                                                 T* __restrict__ out) {
+// The units of a call whose tokens share them: a unit is of one sequence and ends at a multiple of `tokens`.  One workgroup.
+__global__ __launch_bounds__(1024) void list_units_kernel(const int32_t* __restrict__ seq, int n_tokens, int tokens,
+                                                          int32_t* __restrict__ units) {
+    __shared__ int counts[16];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    int base = 0;
+    for (int t0 = 0; t0 < n_tokens; t0 += 1024) {
+        const int t = t0 + tid;
+        const bool first = t < n_tokens && (t % tokens == 0 || seq[t] != seq[t - 1]);
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(first);
+        if (lane == 0) counts[wave] = __popcll(mask);
+        __syncthreads();
+        int at = base + __popcll(mask & ((uint64_t(1) << lane) - 1));
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) at += counts[w];
+            base += counts[w];
+        }
+        if (first) units[1 + at] = t;
+        __syncthreads();
+    }
+    if (tid == 0) {
+        units[0] = base;
+        units[1 + base] = n_tokens;
+    }
+}
+
+// What a wavefront holds of its columns.
+template <int D, int kTiles>
+struct Acc {
+    f32x4 o[kTiles][D / 16];
+    float m[kTiles], l[kTiles];
+};
+
+// A page's scores.
+template <int D, int kTerms, int kTiles>
+__device__ __forceinline__ void page_scores(const Keys<D>& k, const u32x4 (&qf)[kTiles][kTerms][D / 32],
+                                            f32x4 (&sc)[kTiles][4]) {
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt) {
+        const float ks = scale_of(k.s >> (8 * tt) & 255u);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) sc[i][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < D / 32; ++kk) {
+            const uint32_t c = k.c[tt][kk];
+            const u32x4 kf = {decode2<0>(c, ks), decode2<1>(c, ks), decode2<2>(c, ks), decode2<3>(c, ks)};
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int x = 0; x < kTerms; ++x) sc[i][tt] = mfma(kf, qf[i][x][kk], sc[i][tt]);
+        }
+    }
+}
+
+// Its weights under the running reference, four keys of a tile as two words.
+template <int D, int kTerms, int kTiles>
+__device__ __forceinline__ void page_weights(const f32x4 (&sc)[kTiles][4], float scale, Acc<D, kTiles>& acc,
+                                             uint32_t (&w)[kTiles][4][2][kTerms]) {
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+        float top = sc[i][0][0];
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) top = fmaxf(top, sc[i][tt][x]);
+        top = max_groups(top) * scale;
+        const bool grow = top > acc.m[i] + kSlack;
+        if (__builtin_amdgcn_ballot_w64(grow)) {
+            const float alpha = grow ? __builtin_amdgcn_exp2f(acc.m[i] - top) : 1.f;
+            if (grow) acc.m[i] = top;
+            acc.l[i] *= alpha;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) acc.o[i][j] *= alpha;
+        }
+        const float base = acc.m[i] == -INFINITY ? 0.f : acc.m[i];
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+            float pv[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                pv[x] = __builtin_amdgcn_exp2f(fmaf(sc[i][tt][x], scale, -base));
+                acc.l[i] += pv[x];
+            }
+            split2<kTerms>(pv[0], pv[1], w[i][tt][0]);
+            split2<kTerms>(pv[2], pv[3], w[i][tt][1]);
+        }
+    }
+}
+
+// Its weighted values: two half pages of 32 keys (tiles 2u, 2u + 1), the rows of a quad decoded two dimensions at a time,
+// then paired by row.
+template <int D, int kTerms, int kTiles>
+__device__ __forceinline__ void page_values(const Values<D>& v, const uint32_t (&w)[kTiles][4][2][kTerms],
+                                            Acc<D, kTiles>& acc) {
+    constexpr int DL = D / 16;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        uint32_t vf[DL][4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int tt = 2 * u + b;
+#pragma unroll
+            for (int r2 = 0; r2 < 2; ++r2) {
+                uint32_t lo[DL / 2], hi[DL / 2];
+                const float s0 = scale_of(v.s[tt] >> (16 * r2) & 255u);
+                const float s1 = scale_of(v.s[tt] >> (16 * r2 + 8) & 255u);
+                if constexpr (DL == 8) {
+                    const uint32_t c0 = v.c[tt][2 * r2], c1 = v.c[tt][2 * r2 + 1];
+                    lo[0] = decode2<0>(c0, s0);
+                    lo[1] = decode2<1>(c0, s0);
+                    lo[2] = decode2<2>(c0, s0);
+                    lo[3] = decode2<3>(c0, s0);
+                    hi[0] = decode2<0>(c1, s1);
+                    hi[1] = decode2<1>(c1, s1);
+                    hi[2] = decode2<2>(c1, s1);
+                    hi[3] = decode2<3>(c1, s1);
+                } else {
+                    const uint32_t c = v.c[tt][r2];
+                    lo[0] = decode2<0>(c, s0);
+                    lo[1] = decode2<1>(c, s0);
+                    hi[0] = decode2<2>(c, s1);
+                    hi[1] = decode2<3>(c, s1);
+                }
+#pragma unroll
+                for (int j = 0; j < DL / 2; ++j) {
+                    vf[2 * j][2 * b + r2] = __builtin_amdgcn_perm(hi[j], lo[j], 0x05040100u);
+                    vf[2 * j + 1][2 * b + r2] = __builtin_amdgcn_perm(hi[j], lo[j], 0x07060302u);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int x = 0; x < kTerms; ++x) {
+                const u32x4 pf = {w[i][2 * u][0][x], w[i][2 * u][1][x], w[i][2 * u + 1][0][x], w[i][2 * u + 1][1][x]};
+#pragma unroll
+                for (int j = 0; j < DL; ++j)
+                    acc.o[i][j] = mfma(u32x4{vf[j][0], vf[j][1], vf[j][2], vf[j][3]}, pf, acc.o[i][j]);
+            }
+    }
+}
+
+// The weight of a partial result with reference m under the reference `base`.  One without a reference has seen nothing
+// (zeros) or only what is not a number: that stays.
+__device__ __forceinline__ float part_weight(float m, float base) {
+    return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - base);
+}
+__device__ __forceinline__ float natural_lse(float base, float l) {
+    return l == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(l);
+}
+
+// Wavefronts of a SIMD that the registers are kept to (one tile: as many as fit without spills).
+template <typename T, int D, int kTiles>
+constexpr int kResident = kTiles == 2 || (sizeof(T) == 4 && D == 128) ? 2 : sizeof(T) == 2 && D == 64 ? 4 : 3;
+
+template <typename T, int D, int kTiles, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles>)) void attend_tokens_kernel(PoolView pool, TokensView tok, AttendArgs a,
+                                                                    const T* __restrict__ q, int64_t q_stride,
+                                                                    T* __restrict__ out, int grid_units) {
     using F = PageFormat<D>;
+    constexpr int kThreads = 64 * kWaves;
     constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;
     constexpr int DL = F::kLaneDims;
     constexpr int kSteps = D / 32;
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(D));  // log2(e) / sqrt(d)
-    __shared__ float s_o[kWaves][16][D + 4];
-    __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-    const int64_t unit = linear_block<kThreads>();
-    const int t = static_cast<int>(unit / pool.n_kv), h = static_cast<int>(unit % pool.n_kv);
-    if (t >= tok.n_tokens) return;
+    extern __shared__ __align__(16) float smem[];
+    float(*s_o)[16 * kTiles][D + 4] = reinterpret_cast<float(*)[16 * kTiles][D + 4]>(smem);
+    float(*s_m)[16 * kTiles] = reinterpret_cast<float(*)[16 * kTiles]>(smem + kWaves * 16 * kTiles * (D + 4));
+    float(*s_l)[16 * kTiles] = s_m + kWaves;
+    const int n_units = a.units ? a.units[0] : tok.n_tokens;
+    const int64_t block = linear_block<kThreads>();
+    const int split = static_cast<int>(block % a.splits);
+    const int h = static_cast<int>(block / a.splits % pool.n_kv);
+    for (int64_t unit = block / a.splits / pool.n_kv; unit < n_units; unit += grid_units) {
+    const int t = a.units ? a.units[1 + unit] : static_cast<int>(unit);
+    const int n_tok = a.units ? a.units[2 + unit] - t : 1;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, g = lane >> 4;
-    int s = 0, p = 0;
-    const bool in = tok.at(t, s, p);
-    const int n_entries = !in ? 0 : a.list ? a.n_list : p / kPageRows + 1;
-    const int32_t* list = a.list ? a.list + unit * a.n_list : nullptr;
+    const int columns = n_tok * a.ratio;
 
-    // column m: query head m of the KV head's (zeros past the last)
-    u32x4 qf[kTerms][kSteps];
-    {
-        const T* row = q + t * q_stride + (static_cast<int64_t>(h) * a.ratio + m) * D + g * (D / 4);
+    // column 16 i + m: query head column % r of token t + column / r; zeros past the last
+    int pos[kTiles];
+    int s = 0, last = -1, first = INT32_MAX;  // the unit's sequence, its tokens' largest and smallest positions
+    u32x4 qf[kTiles][kTerms][kSteps];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+        const int c = 16 * i + m;
+        const bool real = c < columns;
+        const int tc = t + (real ? c / a.ratio : 0);
+        int sc = 0, pc = 0;
+        const bool in = tok.at(tc, sc, pc);
+        pos[i] = in ? pc : -1;
+        last = max(last, pos[i]);
+        first = min(first, pos[i]);
+        s = in ? sc : s;
+        const T* row = q + tc * q_stride + (static_cast<int64_t>(h) * a.ratio + c % a.ratio) * D + g * (D / 4);
 #pragma unroll
         for (int kk = 0; kk < kSteps; ++kk) {
             float x[8] = {};
-            if (in && m < a.ratio) load8(row + 8 * kk, x);
+            if (real && in) load8(row + 8 * kk, x);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int e = 0; e < 4; ++e) {
                 uint32_t w[kTerms];
-                split2<kTerms>(x[2 * i], x[2 * i + 1], w);
+                split2<kTerms>(x[2 * e], x[2 * e + 1], w);
 #pragma unroll
-                for (int e = 0; e < kTerms; ++e) qf[e][kk][i] = w[e];
+                for (int y = 0; y < kTerms; ++y) qf[i][y][kk][e] = w[y];
             }
         }
     }
-    f32x4 o[DL];
+    if (n_tok > 1) {
 #pragma unroll
-    for (int j = 0; j < DL; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m_run = -INFINITY, l_run = 0.f;
+        for (int x = 1; x < 16; x *= 2) {
+            last = max(last, __shfl_xor(last, x));
+            first = min(first, __shfl_xor(first, x));
+            s = max(s, __shfl_xor(s, x));
+        }
+    }
+    s = __builtin_amdgcn_readfirstlane(s);
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
+    const int32_t* list = a.list ? a.list + (static_cast<int64_t>(t) * pool.n_kv + h) * a.n_list : nullptr;
+    const int n_all = last < 0 ? 0 : list ? a.n_list : last / kPageRows + 1;
+    const int parts = min(a.splits, max(1, (n_all + a.run - 1) / a.run));
+    if (split >= parts) continue;
+    if (a.splits > 1 && split == 0 && h == 0 && tid < n_tok) a.parts[t + tid] = parts;
+    const int n_entries = parts == 1 ? n_all : min(n_all, (split + 1) * a.run);
 
-    for (int e0 = wave; e0 < n_entries; e0 += 64 * kWaves) {
+    Acc<D, kTiles> acc;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+        acc.m[i] = -INFINITY;
+        acc.l[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < DL; ++j) acc.o[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int e0 = split * a.run + wave; e0 < n_entries; e0 += 64 * kWaves) {
         // the next 64 entries of this wavefront, one a lane
         SeenPage mine{-1, 0};
+        int chunk = 0;
         const int e = e0 + lane * kWaves;
-        if (e < n_entries) mine = seen_page(pool, tok, s, p, list ? list[e] : e);
-        const int batch = min(64, (n_entries - e0 + kWaves - 1) / kWaves);
-        for (int i = 0; i < batch; ++i) {
-            const int rows = __builtin_amdgcn_readlane(mine.rows, i);
-            if (rows == 0) continue;
-            const unsigned char* head = pool.page(__builtin_amdgcn_readlane(mine.id, i)) + h * F::kBytes;
-            Page<D> pg;
-            load_page<D>(head, m, g, pg);
-
-            f32x4 sc[4];
-#pragma unroll
-            for (int tt = 0; tt < 4; ++tt) {
-                const float ks = scale_of(pg.ks >> (8 * tt) & 255u);
-                sc[tt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int kk = 0; kk < kSteps; ++kk) {
-                    const uint32_t c = pg.k[tt][kk];
-                    const u32x4 kf = {decode2<0>(c, ks), decode2<1>(c, ks), decode2<2>(c, ks), decode2<3>(c, ks)};
-#pragma unroll
-                    for (int x = 0; x < kTerms; ++x) sc[tt] = mfma(kf, qf[x][kk], sc[tt]);
-                }
-            }
-            if (rows < kPageRows) {  // the token's own page: rows behind it hold anything
+        if (e < n_entries) {
+            chunk = list ? list[e] : e;
+            mine = seen_page(pool, tok, s, last, chunk);
+        }
+        uint64_t left = __builtin_amdgcn_ballot_w64(mine.rows > 0);
+        if (!left) continue;
+        int cur = static_cast<int>(__builtin_ctzll(left));
+        const auto part = [&](int i, bool any) {
+            return make_rsrc(pool.page(__builtin_amdgcn_readlane(mine.id, i)) + h * F::kBytes, any ? F::kBytes : 0);
+        };
+        // keys of the next page are fetched once this one's scores are formed, its values once this one's are used
+        Keys<D> k;
+        Values<D> v;
+        {
+            const buf_rsrc r = part(cur, true);
+            load_keys<D>(r, m, g, k);
+            load_values<D>(r, m, g, v);
+        }
+        while (left) {
+            left &= left - 1;
+            const int next = left ? static_cast<int>(__builtin_ctzll(left)) : cur;
+            const buf_rsrc r = part(next, left != 0);
+            const int c = __builtin_amdgcn_readlane(chunk, cur);
+            f32x4 sc[kTiles][4];
+            page_scores<D, kTerms, kTiles>(k, qf, sc);
+            load_keys<D>(r, m, g, k);
+            if (first < c * kPageRows + kPageRows - 1) {
+                // rows past a column's position are not seen; those behind the last stored one hold anything, whose
+                // values count as some number (times a weight of 0)
+                __asm__ volatile("");  // a branch: most pages need none of this
+                const int rows = __builtin_amdgcn_readlane(mine.rows, cur);
 #pragma unroll
                 for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        if (16 * tt + 4 * g + x >= rows) {
-                            sc[tt][x] = -INFINITY;
-                            pg.vs[tt] = (pg.vs[tt] & ~(255u << (8 * x))) | 127u << (8 * x);
-                        }
-                // codes of an unseen row: zeros, as its weight is (a scale of NaN went above)
-            }
-            float top = sc[0][0];
+                    for (int x = 0; x < 4; ++x) {
+                        const int row = 16 * tt + 4 * g + x;
+                        if (row >= rows) v.s[tt] = (v.s[tt] & ~(255u << (8 * x))) | 127u << (8 * x);
 #pragma unroll
-            for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) top = fmaxf(top, sc[tt][x]);
-            const float m_new = fmaxf(m_run, max_groups(top) * scale);
-            const float m_use = m_new == -INFINITY ? 0.f : m_new;
-            const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
-            m_run = m_new;
-            l_run *= alpha;
-#pragma unroll
-            for (int j = 0; j < DL; ++j) o[j] *= alpha;
-            // weights, four keys of a tile as two words: half page u is tiles 2u, 2u + 1
-            uint32_t w[4][2][kTerms];
-#pragma unroll
-            for (int tt = 0; tt < 4; ++tt) {
-                float pv[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    pv[x] = __builtin_amdgcn_exp2f(fmaf(sc[tt][x], scale, -m_use));
-                    l_run += pv[x];
-                }
-                split2<kTerms>(pv[0], pv[1], w[tt][0]);
-                split2<kTerms>(pv[2], pv[3], w[tt][1]);
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                u32x4 pf[kTerms];
-#pragma unroll
-                for (int x = 0; x < kTerms; ++x)
-                    pf[x] = u32x4{w[2 * u][0][x], w[2 * u][1][x], w[2 * u + 1][0][x], w[2 * u + 1][1][x]};
-                // rows of a quad decoded two dimensions at a time, then paired by row
-                uint32_t vf[DL][4];
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int tt = 2 * u + b;
-#pragma unroll
-                    for (int r2 = 0; r2 < 2; ++r2) {
-                        uint32_t lo[DL / 2], hi[DL / 2];
-                        const float s0 = scale_of(pg.vs[tt] >> (16 * r2) & 255u);
-                        const float s1 = scale_of(pg.vs[tt] >> (16 * r2 + 8) & 255u);
-                        if constexpr (DL == 8) {
-                            const uint32_t c0 = pg.v[tt][2 * r2], c1 = pg.v[tt][2 * r2 + 1];
-                            lo[0] = decode2<0>(c0, s0);
-                            lo[1] = decode2<1>(c0, s0);
-                            lo[2] = decode2<2>(c0, s0);
-                            lo[3] = decode2<3>(c0, s0);
-                            hi[0] = decode2<0>(c1, s1);
-                            hi[1] = decode2<1>(c1, s1);
-                            hi[2] = decode2<2>(c1, s1);
-                            hi[3] = decode2<3>(c1, s1);
-                        } else {
-                            const uint32_t c = pg.v[tt][r2];
-                            lo[0] = decode2<0>(c, s0);
-                            lo[1] = decode2<1>(c, s0);
-                            hi[0] = decode2<2>(c, s1);
-                            hi[1] = decode2<3>(c, s1);
-                        }
-#pragma unroll
-                        for (int j = 0; j < DL / 2; ++j) {
-                            vf[2 * j][2 * b + r2] = __builtin_amdgcn_perm(hi[j], lo[j], 0x05040100u);
-                            vf[2 * j + 1][2 * b + r2] = __builtin_amdgcn_perm(hi[j], lo[j], 0x07060302u);
-                        }
+                        for (int i = 0; i < kTiles; ++i)
+                            if (row > pos[i] - c * kPageRows) sc[i][tt][x] = -INFINITY;
                     }
-                }
-#pragma unroll
-                for (int j = 0; j < DL; ++j) {
-                    const u32x4 va = {vf[j][0], vf[j][1], vf[j][2], vf[j][3]};
-#pragma unroll
-                    for (int x = 0; x < kTerms; ++x) o[j] = mfma(va, pf[x], o[j]);
-                }
             }
+            uint32_t w[kTiles][4][2][kTerms];
+            page_weights<D, kTerms, kTiles>(sc, scale, acc, w);
+            page_values<D, kTerms, kTiles>(v, w, acc);
+            load_values<D>(r, m, g, v);
+            cur = next;
         }
     }
 
-    // join the wavefronts: lane (m, g) holds head m, dimensions (4 g + x) DL + j
-    l_run = sum_groups(l_run);
+    // join the wavefronts: lane (m, g) of tile i holds column 16 i + m, dimensions (4 g + x) DL + j
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+    for (int i = 0; i < kTiles; ++i) {
+        const float l = sum_groups(acc.l[i]);
 #pragma unroll
-        for (int j = 0; j < DL; ++j) s_o[wave][m][(4 * g + x) * DL + j] = o[j][x];
-    if (g == 0) {
-        s_m[wave][m] = m_run;
-        s_l[wave][m] = l_run;
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int j = 0; j < DL; ++j) s_o[wave][16 * i + m][(4 * g + x) * DL + j] = acc.o[i][j][x];
+        if (g == 0) {
+            s_m[wave][16 * i + m] = acc.m[i];
+            s_l[wave][16 * i + m] = l;
+        }
     }
     __syncthreads();
-    for (int i = tid; i < a.ratio * D; i += kThreads) {
+    for (int i = tid; i < columns * D; i += kThreads) {
         const int r = i / D, c = i % D;
         float top = s_m[0][r];
+#pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
-        const float base = top == -INFINITY ? 0.f : top;
-        float l = 0.f, acc = 0.f;
+        const float ref = top == -INFINITY ? 0.f : top;
+        float l = 0.f, sum = 0.f;
+#pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            // a wavefront without a maximum has seen nothing (zeros) or only what is not a number
-            const float f = s_m[w][r] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_m[w][r] - base);
+            const float f = part_weight(s_m[w][r], ref);
             l += f * s_l[w][r];
-            acc += f * s_o[w][r][c];
+            sum += f * s_o[w][r][c];
         }
-        const int64_t row = static_cast<int64_t>(t) * pool.n_kv * a.ratio + h * a.ratio + r;
-        out[row * D + c] = elem<T>::from_f32(l == 0.f ? 0.f : acc / l);
-        if (a.lse && c == 0) a.lse[row] = l == 0.f ? -INFINITY : base * 0.6931471805599453f + logf(l);
+        const int64_t row = static_cast<int64_t>(t + r / a.ratio) * pool.n_kv * a.ratio + h * a.ratio + r % a.ratio;
+        if (parts == 1) {
+            out[row * D + c] = elem<T>::from_f32(l == 0.f ? 0.f : sum / l);
+            if (a.lse && c == 0) a.lse[row] = natural_lse(ref, l);
+        } else {
+            const int64_t at = static_cast<int64_t>(split) * tok.n_tokens * pool.n_kv * a.ratio + row;
+            a.part[at * D + c] = sum;
+            if (c == 0) {
+                a.part_ml[2 * at] = top;
+                a.part_ml[2 * at + 1] = l;
+            }
+        }
+    }
+    __syncthreads();  // LDS is the next unit's
     }
 }
 
+// Joins the partial results of a token's query head, in a fixed order: a workgroup a head, its threads D/4 columns of four
+// dimensions by the groups of parts they add up.
 template <typename T, int D>
-hipError_t run(const PoolView& pool, const TokensView& tok, const AttendArgs& a, const void* q, int64_t q_stride,
-               void* out, hipStream_t stream) {
-    const int64_t n = static_cast<int64_t>(tok.n_tokens) * pool.n_kv;
-    attend_tokens_kernel<T, D><<<grid_of(n, kThreads), kThreads, 0, stream>>>(
-        pool, tok, a, static_cast<const T*>(q), q_stride, static_cast<T*>(out));
+__global__ __launch_bounds__(256) void join_parts_kernel(int n_rows, int heads, AttendArgs a, T* __restrict__ out) {
+    constexpr int kCols = D / 4, kGroups = 256 / kCols;
+    __shared__ float4 s_o[kGroups][kCols];
+    __shared__ float s_l[kGroups], s_m[kGroups];
+    const int64_t row = linear_block<256>();
+    if (row >= n_rows) return;
+    const int parts = a.parts[row / heads];
+    if (parts == 1) return;
+    const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w0 = grp; w0 < parts; w0 += 4 * kGroups) {
+        float2 ml[4];
+        float4 x[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const int64_t at = static_cast<int64_t>(min(w0 + y * kGroups, parts - 1)) * n_rows + row;
+            ml[y] = reinterpret_cast<const float2*>(a.part_ml)[at];
+            x[y] = reinterpret_cast<const float4*>(a.part)[at * kCols + col];
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            if (w0 + y * kGroups >= parts) break;
+            const float top = fmaxf(m, ml[y].x), ref = top == -INFINITY ? 0.f : top;
+            const float f = part_weight(m, ref), e = part_weight(ml[y].x, ref);
+            m = top;
+            l = l * f + ml[y].y * e;
+            o.x = o.x * f + x[y].x * e;
+            o.y = o.y * f + x[y].y * e;
+            o.z = o.z * f + x[y].z * e;
+            o.w = o.w * f + x[y].w * e;
+        }
+    }
+    s_o[grp][col] = o;
+    if (col == 0) {
+        s_m[grp] = m;
+        s_l[grp] = l;
+    }
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    float top = s_m[0];
+#pragma unroll
+    for (int w = 1; w < kGroups; ++w) top = fmaxf(top, s_m[w]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kGroups; ++w) {
+        const float f = part_weight(s_m[w], ref);
+        l += f * s_l[w];
+        sum += f * reinterpret_cast<const float*>(s_o[w])[threadIdx.x];
+    }
+    out[row * D + threadIdx.x] = elem<T>::from_f32(l == 0.f ? 0.f : sum / l);
+    if (a.lse && threadIdx.x == 0) a.lse[row] = natural_lse(ref, l);
+}
+
+template <typename T, int D, int kTiles, int kWaves>
+hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const AttendArgs& a, const void* q,
+               int64_t q_stride, void* out, int grid_units, hipStream_t stream) {
+    constexpr int kThreads = 64 * kWaves;
+    constexpr size_t lds = sizeof(float) * kWaves * 16 * kTiles * (D + 4 + 2);
+    if (lds > 65536) {
+        static std::atomic<uint64_t> done{0};
+        const hipError_t e = once_per_device(done, plan.device, [] {
+            return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_tokens_kernel<T, D, kTiles, kWaves>),
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+        });
+        if (e != hipSuccess) return e;
+    }
+    const int64_t n = static_cast<int64_t>(grid_units) * pool.n_kv * a.splits;
+    attend_tokens_kernel<T, D, kTiles, kWaves><<<grid_of(n, kThreads), kThreads, lds, stream>>>(
+        pool, tok, a, static_cast<const T*>(q), q_stride, static_cast<T*>(out), grid_units);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int heads = pool.n_kv * a.ratio, rows = tok.n_tokens * heads;
+    join_parts_kernel<T, D><<<grid_of(rows, 256), 256, 0, stream>>>(rows, heads, a, static_cast<T*>(out));
     return hipGetLastError();
+}
+
+// How a call is cut: tokens of a unit and their tiles, pages of a workgroup, workgroups of a unit, their wavefronts; and the
+// workspace that takes, in bytes from its start.
+struct Cut {
+    int tokens, tiles, run, splits, waves, grid_units;
+    int64_t parts, part, part_ml, bytes;
+};
+
+int64_t pad16(int64_t n) { return (n + 15) / 16 * 16; }
+
+Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int n_list, int64_t ws_bytes) {
+    const int ratio = plan.p.n_q_heads / plan.p.n_kv_heads;
+    const int64_t rows = static_cast<int64_t>(n_tokens) * plan.p.n_q_heads;
+    Cut c{1, 1, 0, 1, 4, n_tokens, 0, 0, 0, 0};
+    const int64_t entries = std::max(n_list ? n_list : max_pages, 1);
+    // tokens of one sequence share its pages unless they have lists of their own
+    const int per_seq = n_list || n_seqs < 1 ? 1 : static_cast<int>((static_cast<int64_t>(n_tokens) + n_seqs - 1) / n_seqs);
+    const int64_t list_bytes = pad16((static_cast<int64_t>(n_tokens) + 2) * 4);
+    if (per_seq > 1 && ws_bytes >= list_bytes) {
+        // two tiles where one does not hold a sequence's tokens, but for fp32 at 128 dimensions (registers)
+        c.tiles = per_seq * ratio > 16 && !(plan.p.dtype == HGA_F32 && plan.p.head_dim == 128) ? 2 : 1;
+        c.tokens = std::min(per_seq, 16 * c.tiles / ratio);
+        if (c.tokens > 1) {
+            c.grid_units = static_cast<int>(std::min<int64_t>(n_tokens, (n_tokens + c.tokens - 1) / c.tokens + int64_t(n_seqs)));
+            c.bytes = list_bytes;
+        }
+    }
+    const int64_t units = static_cast<int64_t>((n_tokens + c.tokens - 1) / c.tokens) * plan.p.n_kv_heads;
+    c.run = static_cast<int>(entries);
+    const int64_t want = 4 * static_cast<int64_t>(plan.n_cu);
+    if (entries > 64 && units < want) {
+        const int64_t run = std::max<int64_t>(16, (units * entries + want - 1) / want);
+        const int64_t counts = pad16(int64_t(n_tokens) * 4);
+        const int64_t split_bytes = pad16(rows * plan.p.head_dim * 4) + pad16(rows * 8);
+        const int64_t splits = std::min((entries + run - 1) / run, (ws_bytes - c.bytes - counts) / split_bytes);
+        if (splits > 1) {
+            c.splits = static_cast<int>(splits);
+            c.run = static_cast<int>((entries + splits - 1) / splits);
+            c.parts = c.bytes;
+            c.part = c.parts + counts;
+            c.part_ml = c.part + splits * rows * plan.p.head_dim * 4;
+            c.bytes += counts + splits * split_bytes;
+        }
+    }
+    if (c.tiles == 1 && units * c.splits < 2 * plan.n_cu) c.waves = 8;
+    return c;
 }
 
 }  // namespace
 
-int64_t attend_tokens_bytes(const hga_plan&, int, int, int, int) { return 0; }
+int64_t attend_tokens_bytes(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int n_list) {
+    if (n_tokens == 0) return 0;
+    const Cut c = cut_call(plan, n_tokens, n_seqs, max_pages, n_list, INT64_MAX);
+    return c.bytes;
+}
 
 hipError_t launch_attend_tokens(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const void* q,
-                                int64_t q_stride, const int32_t* list, int n_list, void* out, float* lse, void*, int64_t,
-                                hipStream_t stream) {
+                                int64_t q_stride, const int32_t* list, int n_list, void* out, float* lse, void* ws,
+                                int64_t ws_bytes, hipStream_t stream) {
+    const Cut c = cut_call(plan, tok.n_tokens, tok.n_seqs, tok.max_pages, n_list, ws_bytes);
     AttendArgs a;
     a.list = list;
     a.n_list = n_list;
     a.ratio = plan.p.n_q_heads / plan.p.n_kv_heads;
+    a.run = c.run;
+    a.splits = c.splits;
     a.lse = lse;
+    char* w = static_cast<char*>(ws);
+    int32_t* units = c.tokens > 1 ? reinterpret_cast<int32_t*>(w) : nullptr;
+    a.units = units;
+    a.parts = reinterpret_cast<int32_t*>(w + c.parts);
+    a.part = reinterpret_cast<float*>(w + c.part);
+    a.part_ml = reinterpret_cast<float*>(w + c.part_ml);
+    if (units) {
+        list_units_kernel<<<1, 1024, 0, stream>>>(tok.seq, tok.n_tokens, c.tokens, units);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const auto go = [&](auto zero, auto dim) {
+        using T = decltype(zero);
+        constexpr int D = decltype(dim)::value;
+        constexpr int kTwo = sizeof(T) == 4 && D == 128 ? 1 : 2;
+        const auto f = c.tiles == 2 ? run<T, D, kTwo, 4> : c.waves == 8 ? run<T, D, 1, 8> : run<T, D, 1, 4>;
+        return f(plan, pool, tok, a, q, q_stride, out, c.grid_units, stream);
+    };
     const bool f32 = plan.p.dtype == HGA_F32;
-    const auto f = plan.p.head_dim == 128 ? (f32 ? run<float, 128> : run<bf16_t, 128>)
-                                          : (f32 ? run<float, 64> : run<bf16_t, 64>);
-    return f(pool, tok, a, q, q_stride, out, stream);
+    if (plan.p.head_dim == 128)
+        return f32 ? go(0.f, std::integral_constant<int, 128>()) : go(bf16_t(0), std::integral_constant<int, 128>());
+    return f32 ? go(0.f, std::integral_constant<int, 64>()) : go(bf16_t(0), std::integral_constant<int, 64>());
 }
 
 }  // namespace hga
