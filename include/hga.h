@@ -673,7 +673,8 @@ hga_status hga_cache_append(const hga_plan* plan, const hga_pool* pool, int32_t 
 hga_status hga_cache_read(const hga_plan* plan, const hga_pool* pool, int32_t layer,
                           const hga_tokens* tokens, void* k_out, void* v_out, void* stream);
 
-/* Bytes hga_route_tokens needs (0 up to 16384 pages), or a negative
+/* Bytes hga_route_tokens makes use of (up to 16384 pages it does without them,
+ * but takes longer over long histories of few tokens), or a negative
  * hga_status.  Host only. */
 int64_t hga_route_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int32_t max_pages);
 
@@ -687,9 +688,9 @@ int64_t hga_route_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int32
  *   q           [n_tokens][n_q_heads][head_dim] plan dtype (strided)
  *   chunk_list  int32 [n_tokens][n_kv_heads][n_list], ascending, padded with
  *               -1 (all of an idle token's); n_list >= hga_token_list_size
- *   workspace   hga_route_tokens_workspace bytes, or NULL and 0; calls that
- *               overlap in time (graphs replayed side by side among them) need
- *               one each */
+ *   workspace   hga_route_tokens_workspace bytes, or (up to 16384 pages) NULL
+ *               and 0; calls that overlap in time (graphs replayed side by side
+ *               among them) need one each.  The lists do not depend on it. */
 hga_status hga_route_tokens(const hga_plan* plan, const hga_pool* pool, int32_t layer,
                             const hga_tokens* tokens, const void* q, int64_t q_stride,
                             int32_t* chunk_list, int32_t n_list, void* workspace,

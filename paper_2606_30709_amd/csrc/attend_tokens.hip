@@ -278,11 +278,12 @@ __device__ __forceinline__ float natural_lse(float base, float l) {
 }
 
 // Wavefronts of a SIMD that the registers are kept to (one tile: as many as fit without spills).
-template <typename T, int D, int kTiles>
-constexpr int kResident = kTiles == 2 || (sizeof(T) == 4 && D == 128) ? 2 : sizeof(T) == 2 && D == 64 ? 4 : 3;
+template <typename T, int D, int kTiles, bool kShared>
+constexpr int kResident = kTiles == 2 || (sizeof(T) == 4 && D == 128) ? 2 : kShared ? 2 : sizeof(T) == 2 && D == 64 ? 4 : 3;
 
-template <typename T, int D, int kTiles, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles>)) void attend_tokens_kernel(PoolView pool, TokensView tok, AttendArgs a,
+// kShared: units of several tokens, from a.units, of which a workgroup may take more than one; else every token is a unit.
+template <typename T, int D, int kTiles, int kWaves, bool kShared>
+__global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared>)) void attend_tokens_kernel(PoolView pool, TokensView tok, AttendArgs a,
                                                                     const T* __restrict__ q, int64_t q_stride,
                                                                     T* __restrict__ out, int grid_units) {
     using F = PageFormat<D>;
@@ -295,13 +296,16 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles>)) void attend
     float(*s_o)[16 * kTiles][D + 4] = reinterpret_cast<float(*)[16 * kTiles][D + 4]>(smem);
     float(*s_m)[16 * kTiles] = reinterpret_cast<float(*)[16 * kTiles]>(smem + kWaves * 16 * kTiles * (D + 4));
     float(*s_l)[16 * kTiles] = s_m + kWaves;
-    const int n_units = a.units ? a.units[0] : tok.n_tokens;
+    const int n_units = kShared ? a.units[0] : tok.n_tokens;
     const int64_t block = linear_block<kThreads>();
-    const int split = static_cast<int>(block % a.splits);
-    const int h = static_cast<int>(block / a.splits % pool.n_kv);
-    for (int64_t unit = block / a.splits / pool.n_kv; unit < n_units; unit += grid_units) {
-    const int t = a.units ? a.units[1 + unit] : static_cast<int>(unit);
-    const int n_tok = a.units ? a.units[2 + unit] - t : 1;
+    // splits in the outer order: short histories have none of the later ones, and a split as the inner one would be an XCD
+    const int64_t row = static_cast<int64_t>(grid_units) * pool.n_kv;
+    const int split = static_cast<int>(block / row);
+    const int h = static_cast<int>(block % pool.n_kv);
+    if (split >= a.splits) return;
+    for (int64_t unit = block % row / pool.n_kv; unit < n_units; unit += grid_units) {
+    const int t = kShared ? a.units[1 + unit] : static_cast<int>(unit);
+    const int n_tok = kShared ? a.units[2 + unit] - t : 1;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, g = lane >> 4;
     const int columns = n_tok * a.ratio;
 
@@ -334,7 +338,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles>)) void attend
             }
         }
     }
-    if (n_tok > 1) {
+    if (kShared) {
 #pragma unroll
         for (int x = 1; x < 16; x *= 2) {
             last = max(last, __shfl_xor(last, x));
@@ -348,7 +352,10 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles>)) void attend
     const int32_t* list = a.list ? a.list + (static_cast<int64_t>(t) * pool.n_kv + h) * a.n_list : nullptr;
     const int n_all = last < 0 ? 0 : list ? a.n_list : last / kPageRows + 1;
     const int parts = min(a.splits, max(1, (n_all + a.run - 1) / a.run));
-    if (split >= parts) continue;
+    if (split >= parts) {
+        if (!kShared) break;
+        continue;
+    }
     if (a.splits > 1 && split == 0 && h == 0 && tid < n_tok) a.parts[t + tid] = parts;
     const int n_entries = parts == 1 ? n_all : min(n_all, (split + 1) * a.run);
 
@@ -391,7 +398,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles>)) void attend
             f32x4 sc[kTiles][4];
             page_scores<D, kTerms, kTiles>(k, qf, sc);
             load_keys<D>(r, m, g, k);
-            if (first < c * kPageRows + kPageRows - 1) {
+            if (kShared ? first < c * kPageRows + kPageRows - 1 : __builtin_amdgcn_readlane(mine.rows, cur) < kPageRows) {
                 // rows past a column's position are not seen; those behind the last stored one hold anything, whose
                 // values count as some number (times a weight of 0)
                 __asm__ volatile("");  // a branch: most pages need none of this
@@ -404,7 +411,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles>)) void attend
                         if (row >= rows) v.s[tt] = (v.s[tt] & ~(255u << (8 * x))) | 127u << (8 * x);
 #pragma unroll
                         for (int i = 0; i < kTiles; ++i)
-                            if (row > pos[i] - c * kPageRows) sc[i][tt][x] = -INFINITY;
+                            if (kShared ? row > pos[i] - c * kPageRows : row >= rows) sc[i][tt][x] = -INFINITY;
                     }
             }
             uint32_t w[kTiles][4][2][kTerms];
@@ -442,12 +449,12 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles>)) void attend
             l += f * s_l[w][r];
             sum += f * s_o[w][r][c];
         }
-        const int64_t row = static_cast<int64_t>(t + r / a.ratio) * pool.n_kv * a.ratio + h * a.ratio + r % a.ratio;
+        const int64_t at_row = static_cast<int64_t>(t + r / a.ratio) * pool.n_kv * a.ratio + h * a.ratio + r % a.ratio;
         if (parts == 1) {
-            out[row * D + c] = elem<T>::from_f32(l == 0.f ? 0.f : sum / l);
-            if (a.lse && c == 0) a.lse[row] = natural_lse(ref, l);
+            out[at_row * D + c] = elem<T>::from_f32(l == 0.f ? 0.f : sum / l);
+            if (a.lse && c == 0) a.lse[at_row] = natural_lse(ref, l);
         } else {
-            const int64_t at = static_cast<int64_t>(split) * tok.n_tokens * pool.n_kv * a.ratio + row;
+            const int64_t at = static_cast<int64_t>(split) * tok.n_tokens * pool.n_kv * a.ratio + at_row;
             a.part[at * D + c] = sum;
             if (c == 0) {
                 a.part_ml[2 * at] = top;
@@ -455,6 +462,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles>)) void attend
             }
         }
     }
+    if (!kShared) break;
     __syncthreads();  // LDS is the next unit's
     }
 }
@@ -518,7 +526,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(int n_rows, int heads, 
     if (a.lse && threadIdx.x == 0) a.lse[row] = natural_lse(ref, l);
 }
 
-template <typename T, int D, int kTiles, int kWaves>
+template <typename T, int D, int kTiles, int kWaves, bool kShared>
 hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const AttendArgs& a, const void* q,
                int64_t q_stride, void* out, int grid_units, hipStream_t stream) {
     constexpr int kThreads = 64 * kWaves;
@@ -526,13 +534,13 @@ hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok
     if (lds > 65536) {
         static std::atomic<uint64_t> done{0};
         const hipError_t e = once_per_device(done, plan.device, [] {
-            return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_tokens_kernel<T, D, kTiles, kWaves>),
+            return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_tokens_kernel<T, D, kTiles, kWaves, kShared>),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
         });
         if (e != hipSuccess) return e;
     }
     const int64_t n = static_cast<int64_t>(grid_units) * pool.n_kv * a.splits;
-    attend_tokens_kernel<T, D, kTiles, kWaves><<<grid_of(n, kThreads), kThreads, lds, stream>>>(
+    attend_tokens_kernel<T, D, kTiles, kWaves, kShared><<<grid_of(n, kThreads), kThreads, lds, stream>>>(
         pool, tok, a, static_cast<const T*>(q), q_stride, static_cast<T*>(out), grid_units);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
@@ -569,7 +577,9 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
     }
     const int64_t units = static_cast<int64_t>((n_tokens + c.tokens - 1) / c.tokens) * plan.p.n_kv_heads;
     c.run = static_cast<int>(entries);
-    const int64_t want = 4 * static_cast<int64_t>(plan.n_cu);
+    // workgroups that the device holds at once or a few more (decode of 32 histories up to 32K, 4 heads of d128: 68 us with 4
+    // a CU, 72-78 with 2, 3, 6 or 8; 512 tokens of a 16K prompt in two tiles: 171 us with 2, 186 with 4)
+    const int64_t want = (c.tiles == 2 ? 2 : 4) * static_cast<int64_t>(plan.n_cu);
     if (entries > 64 && units < want) {
         const int64_t run = std::max<int64_t>(16, (units * entries + want - 1) / want);
         const int64_t counts = pad16(int64_t(n_tokens) * 4);
@@ -622,7 +632,9 @@ hipError_t launch_attend_tokens(const hga_plan& plan, const PoolView& pool, cons
         using T = decltype(zero);
         constexpr int D = decltype(dim)::value;
         constexpr int kTwo = sizeof(T) == 4 && D == 128 ? 1 : 2;
-        const auto f = c.tiles == 2 ? run<T, D, kTwo, 4> : c.waves == 8 ? run<T, D, 1, 8> : run<T, D, 1, 4>;
+        const auto f = c.tokens > 1 ? (c.tiles == 2 ? run<T, D, kTwo, 4, true>
+                                       : c.waves == 8 ? run<T, D, 1, 8, true> : run<T, D, 1, 4, true>)
+                                    : c.waves == 8 ? run<T, D, 1, 8, false> : run<T, D, 1, 4, false>;
         return f(plan, pool, tok, a, q, q_stride, out, c.grid_units, stream);
     };
     const bool f32 = plan.p.dtype == HGA_F32;

@@ -72,7 +72,7 @@ hga_status check_counts(const hga_plan* plan, int32_t n_tokens, int32_t n_seqs, 
     return HGA_OK;
 }
 
-hga_status view_tokens(const hga_plan* plan, const hga_tokens* tok, hga::TokensView* v) {
+hga_status view_tokens(const hga_plan* plan, const hga_tokens* tok, const hga::PoolView& pool, hga::TokensView* v) {
     if (!tok) return fail(HGA_EINVAL, "tokens is NULL");
     HGA_TRY(check_counts(plan, tok->n_tokens, tok->n_seqs, tok->max_pages));
     if (tok->n_tokens > 0) {
@@ -81,6 +81,8 @@ hga_status view_tokens(const hga_plan* plan, const hga_tokens* tok, hga::TokensV
         if (tok->n_seqs > 0 && tok->max_pages > 0) HGA_TRY(check_index(tok->page_table, "tokens.page_table"));
     }
     *v = hga::TokensView{tok->tok_seq, tok->tok_pos, tok->page_table, tok->n_tokens, tok->n_seqs, tok->max_pages};
+    // without a page every one is absent, and so every token as an idle one; the kernels count on a first page
+    if (static_cast<int64_t>(pool.n_hot) + pool.n_cold == 0) v->max_pages = 0;
     return HGA_OK;
 }
 
@@ -124,7 +126,7 @@ hga_status hga_cache_append(const hga_plan* plan, const hga_pool* pool, int32_t 
     hga::PoolView pv;
     hga::TokensView tv;
     HGA_TRY(view_pool(plan, pool, layer, &pv));
-    HGA_TRY(view_tokens(plan, tokens, &tv));
+    HGA_TRY(view_tokens(plan, tokens, pv, &tv));
     if (tv.n_tokens == 0) return HGA_OK;
     HGA_TRY(check_rows(plan, k, k_stride, plan->p.n_kv_heads, "k"));
     HGA_TRY(check_rows(plan, v, v_stride, plan->p.n_kv_heads, "v"));
@@ -139,7 +141,7 @@ hga_status hga_cache_read(const hga_plan* plan, const hga_pool* pool, int32_t la
     hga::PoolView pv;
     hga::TokensView tv;
     HGA_TRY(view_pool(plan, pool, layer, &pv));
-    HGA_TRY(view_tokens(plan, tokens, &tv));
+    HGA_TRY(view_tokens(plan, tokens, pv, &tv));
     if (tv.n_tokens == 0) return HGA_OK;
     HGA_TRY(check_tensor(k_out, "k_out"));
     HGA_TRY(check_tensor(v_out, "v_out"));
@@ -151,7 +153,7 @@ hga_status hga_cache_read(const hga_plan* plan, const hga_pool* pool, int32_t la
 int64_t hga_route_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int32_t max_pages) {
     if (!plan) return fail(HGA_EINVAL, "plan is NULL");
     HGA_TRY(check_counts(plan, n_tokens, 0, max_pages));
-    return hga::route_tokens_bytes(*plan, n_tokens, max_pages);
+    return hga::route_tokens_bytes(*plan, n_tokens, max_pages, false);
 }
 
 hga_status hga_route_tokens(const hga_plan* plan, const hga_pool* pool, int32_t layer, const hga_tokens* tokens,
@@ -161,7 +163,7 @@ hga_status hga_route_tokens(const hga_plan* plan, const hga_pool* pool, int32_t 
     hga::PoolView pv;
     hga::TokensView tv;
     HGA_TRY(view_pool(plan, pool, layer, &pv));
-    HGA_TRY(view_tokens(plan, tokens, &tv));
+    HGA_TRY(view_tokens(plan, tokens, pv, &tv));
     if (n_list < list_size(plan))
         return fail(HGA_EINVAL, "n_list %d is below the %lld chunks a token may list", n_list,
                     static_cast<long long>(list_size(plan)));
@@ -169,13 +171,13 @@ hga_status hga_route_tokens(const hga_plan* plan, const hga_pool* pool, int32_t 
     if (tv.n_tokens == 0) return HGA_OK;
     HGA_TRY(check_rows(plan, q, q_stride, plan->p.n_q_heads, "q"));
     HGA_TRY(check_index(chunk_list, "chunk_list"));
-    const int64_t need = hga::route_tokens_bytes(*plan, tv.n_tokens, tv.max_pages);
+    const int64_t need = hga::route_tokens_bytes(*plan, tv.n_tokens, tv.max_pages, true);
     if (workspace_bytes < need)
         return fail(HGA_EINVAL, "workspace of %lld bytes is below the %lld needed",
                     static_cast<long long>(workspace_bytes), static_cast<long long>(need));
     clear_stale_error();
     return launched(hga::launch_route_tokens(*plan, pv, tv, q, q_stride, chunk_list, n_list, workspace,
-                                             static_cast<hipStream_t>(stream)),
+                                             workspace_bytes, static_cast<hipStream_t>(stream)),
                     "hga_route_tokens launch");
 }
 
@@ -194,7 +196,7 @@ hga_status hga_attend_tokens(const hga_plan* plan, const hga_pool* pool, int32_t
     hga::PoolView pv;
     hga::TokensView tv;
     HGA_TRY(view_pool(plan, pool, layer, &pv));
-    HGA_TRY(view_tokens(plan, tokens, &tv));
+    HGA_TRY(view_tokens(plan, tokens, pv, &tv));
     if (n_list < 0 || (chunk_list != nullptr) != (n_list > 0))
         return fail(HGA_EINVAL, "chunk_list and n_list: a list of n_list >= 1 entries, or NULL and 0");
     HGA_TRY(check_workspace(workspace, workspace_bytes));

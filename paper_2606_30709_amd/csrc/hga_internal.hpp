@@ -211,11 +211,12 @@ int64_t copy_pages_workgroups(const hga_plan& plan);  // of one page in one laye
 hipError_t launch_copy_pages(const hga_plan& plan, const hga_pool& pool, void* cold,
                              const int32_t* src, const int32_t* dst, int n, hipStream_t stream);
 
-// Routing of single tokens to pages, and its workspace's bytes.
-int64_t route_tokens_bytes(const hga_plan& plan, int n_tokens, int max_pages);
+// Routing of single tokens to pages, and the workspace bytes it makes use of
+// (or cannot do without).
+int64_t route_tokens_bytes(const hga_plan& plan, int n_tokens, int max_pages, bool must);
 hipError_t launch_route_tokens(const hga_plan& plan, const PoolView& pool, const TokensView& tok,
                                const void* q, int64_t q_stride, int32_t* list, int n_list, void* ws,
-                               hipStream_t stream);
+                               int64_t ws_bytes, hipStream_t stream);
 
 // Attention of single tokens over listed pages (list NULL: all), and the
 // bytes its workspace may take.

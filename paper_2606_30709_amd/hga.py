@@ -512,8 +512,14 @@ def _require(ok, message: str):
         raise HgaError(-1, f"HGA_EINVAL: {message}")
 
 
-def _expect(t, name: str, dtype, shape, device=None, contiguous=True):
-    """A tensor argument as the call takes it (None in shape: any size)."""
+def _expect(t, name: str, dtype, shape: tuple, device=None, contiguous=True):
+    """A tensor argument as the call takes it (None in shape: any size).  A
+    decode step makes these checks a few times a layer: what is right passes
+    without looking further."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and (device is None or t.device == device)
+            and (not contiguous or t.is_contiguous())):
+        return
     _require(isinstance(t, torch.Tensor), f"{name} must be a tensor")
     _require(t.dtype == dtype, f"{name} must be {dtype}, is {t.dtype}")
     _require(t.dim() == len(shape) and all(w is None or w == n for n, w in zip(t.shape, shape)),
@@ -527,10 +533,29 @@ def _rows(t, name: str, plan: Plan, n_tokens: int, heads: int, device) -> int:
     """Elements from a token's row to the next of t [n_tokens, heads, head_dim]."""
     d = plan.params.head_dim
     _expect(t, name, plan.torch_dtype, (n_tokens, heads, d), device, contiguous=False)
-    _require(n_tokens == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d)),
+    row, head, one = t.stride()
+    _require(n_tokens == 0 or (one == 1 and (heads == 1 or head == d)),
              f"{name}: a token's heads must be contiguous")
     # a single token's stride means nothing (and may be anything)
-    return t.stride(0) if n_tokens > 1 else heads * d
+    return row if n_tokens > 1 else heads * d
+
+
+def _space(workspace, device):
+    if workspace is None:
+        return None, 0
+    _require(workspace.is_contiguous() and workspace.device == device,
+             f"workspace must be a contiguous tensor on {device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _on(pool, stream):
+    """The stream to launch on: given, or the current one of the pool's device,
+    which must be the current device."""
+    _require(pool.index == torch.cuda.current_device(),
+             f"the pool is on {pool.device}, the current device is {torch.cuda.current_device()}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(pool.index)
+    return _stream(stream)
 
 
 class Pool:
@@ -564,7 +589,7 @@ class Pool:
                 (n_layers, n_pages + n_cold, p.n_kv_heads, p.head_dim), pages.device)
         self.pages, self.page_sum, self.cold = pages, page_sum, cold
         self.n_layers, self.n_pages, self.n_cold = n_layers, n_pages, n_cold
-        self.device = pages.device
+        self.device, self.index = pages.device, pages.device.index
         self.struct = HgaPool(pages.data_ptr(), None if cold is None else cold.data_ptr(),
                               page_sum.data_ptr(), n_layers, n_pages, n_cold)
 
@@ -584,7 +609,7 @@ class TokenBatch:
         self.tok_seq, self.tok_pos, self.page_table = tok_seq, tok_pos, page_table
         self.n_tokens = tok_seq.shape[0]
         self.n_seqs, self.max_pages = page_table.shape
-        self.device = dev
+        self.device, self.index = dev, dev.index
         self.struct = HgaTokens(tok_seq.data_ptr(), tok_pos.data_ptr(), page_table.data_ptr(),
                                 self.n_tokens, self.n_seqs, self.max_pages)
 
@@ -596,14 +621,8 @@ def _size(n: int) -> int:
 
 
 def _same_device(pool: Pool, batch: TokenBatch):
-    _require(pool.device == batch.device,
+    _require(pool.index == batch.index,
              f"the batch is on {batch.device}, the pool on {pool.device}")
-    _on_current(pool)
-
-
-def _on_current(pool: Pool):
-    _require(pool.device.index == torch.cuda.current_device(),
-             f"the pool is on {pool.device}, the current device is {torch.cuda.current_device()}")
 
 
 def hga_page_bytes(plan: Plan) -> int:
@@ -625,7 +644,7 @@ def hga_cache_append(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, k, v
     vs = _rows(v, "v", plan, batch.n_tokens, kv, dev)
     _check(library().hga_cache_append(
         plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct), _ptr(k), ks,
-        _ptr(v), vs, _stream(stream)))
+        _ptr(v), vs, _on(pool, stream)))
 
 
 def hga_cache_read(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, k_out, v_out,
@@ -638,11 +657,11 @@ def hga_cache_read(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, k_out,
     _expect(v_out, "v_out", plan.torch_dtype, shape, pool.device)
     _check(library().hga_cache_read(
         plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct), _ptr(k_out),
-        _ptr(v_out), _stream(stream)))
+        _ptr(v_out), _on(pool, stream)))
 
 
 def hga_route_tokens_workspace(plan: Plan, batch: TokenBatch) -> int:
-    """Bytes of workspace hga_route_tokens needs for the batch (often 0)."""
+    """Bytes of workspace hga_route_tokens makes use of for the batch (often 0)."""
     return _size(library().hga_route_tokens_workspace(plan.handle, batch.n_tokens,
                                                       batch.max_pages))
 
@@ -655,10 +674,10 @@ def hga_route_tokens(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, q, c
     _same_device(pool, batch)
     qs = _rows(q, "q", plan, batch.n_tokens, plan.params.n_q_heads, pool.device)
     _expect(chunk_list, "chunk_list", torch.int32,
-            (batch.n_tokens, plan.params.n_kv_heads, None), pool.device)
+            (batch.n_tokens, plan.params.n_kv_heads, chunk_list.shape[-1]), pool.device)
     _check(library().hga_route_tokens(
         plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct), _ptr(q), qs,
-        _ptr(chunk_list), chunk_list.shape[2], *_ws(workspace), _stream(stream)))
+        _ptr(chunk_list), chunk_list.shape[2], *_space(workspace, pool.device), _on(pool, stream)))
 
 
 def hga_attend_tokens_workspace(plan: Plan, batch: TokenBatch, chunk_list=None) -> int:
@@ -682,20 +701,19 @@ def hga_attend_tokens(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, q, 
         _expect(lse, "lse", torch.float32, (batch.n_tokens, p.n_q_heads), pool.device)
     n_list = 0
     if chunk_list is not None:
-        _expect(chunk_list, "chunk_list", torch.int32, (batch.n_tokens, p.n_kv_heads, None),
+        n_list = chunk_list.shape[-1]
+        _expect(chunk_list, "chunk_list", torch.int32, (batch.n_tokens, p.n_kv_heads, n_list),
                 pool.device)
-        n_list = chunk_list.shape[2]
         _require(n_list > 0, "chunk_list must hold an entry a token")
     _check(library().hga_attend_tokens(
         plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct), _ptr(q), qs,
-        _ptr(chunk_list), n_list, _ptr(out), _ptr(lse), *_ws(workspace), _stream(stream)))
+        _ptr(chunk_list), n_list, _ptr(out), _ptr(lse), *_space(workspace, pool.device), _on(pool, stream)))
 
 
 def hga_copy_pages(plan: Plan, pool: Pool, src, dst, stream=None):
     """Copies page src[i] over page dst[i] (int32 [n], on the GPU) in every
     layer, summaries included."""
-    _on_current(pool)
     _expect(src, "src", torch.int32, (None,), pool.device)
     _expect(dst, "dst", torch.int32, (src.shape[0],), pool.device)
     _check(library().hga_copy_pages(plan.handle, ctypes.byref(pool.struct), _ptr(src), _ptr(dst),
-                                    src.shape[0], _stream(stream)))
+                                    src.shape[0], _on(pool, stream)))

@@ -174,6 +174,9 @@ def test_listed_chunks(hga, dtype, d, kv, ratio, first, last, prev, topk):
     # padded heads behind the queries: strided rows; a wider list
     wide = sc.random(len(seq), sc.hq + 2, d)
     _route_check(sc, batch, wide[:, :sc.hq], extra=5)
+    # few tokens of long histories
+    batch = sc.batch([4], [4999])
+    _route_check(sc, batch, wide[:1, :sc.hq])
 
 
 def test_a_prompts_tokens_route_alone(hga):
@@ -421,6 +424,15 @@ def test_no_tokens_and_empty_tables(hga):
             out, lse = sc.attend(b, q)
             assert (out == 0).all() and (lse == -np.inf).all()
     hga.hga_copy_pages(sc.plan, sc.pool, b.tok_seq[:0], b.tok_seq[:0])
+    # a pool without a page
+    none = hga.Pool(sc.plan, 0)
+    b = sc.batch([0, 0], [69, 5])
+    sc.pool = none
+    hga.hga_cache_append(sc.plan, none, 0, b, q[:, :2], q[:, :2])
+    assert (sc.route(b, q) == -1).all()
+    out, lse = sc.attend(b, q)
+    assert (out == 0).all() and (lse == -np.inf).all()
+    hga.hga_copy_pages(sc.plan, none, b.tok_seq, b.tok_pos)
 
 
 def test_refusals(hga):

@@ -32,9 +32,9 @@ hipError_t launch_cache_append(const hga_plan&, const PoolView&, const TokensVie
 hipError_t launch_cache_read(const hga_plan&, const PoolView&, const TokensView&, void*, void*, hipStream_t) { return count(); }
 int64_t copy_pages_workgroups(const hga_plan&) { return 4; }
 hipError_t launch_copy_pages(const hga_plan&, const hga_pool&, void*, const int32_t*, const int32_t*, int, hipStream_t) { return count(); }
-int64_t route_tokens_bytes(const hga_plan&, int, int max_pages) { return max_pages > 100 ? 64 : 0; }
+int64_t route_tokens_bytes(const hga_plan&, int, int max_pages, bool) { return max_pages > 100 ? 64 : 0; }
 hipError_t launch_route_tokens(const hga_plan&, const PoolView&, const TokensView&, const void*, int64_t, int32_t*, int,
-                               void*, hipStream_t) { return count(); }
+                               void*, int64_t, hipStream_t) { return count(); }
 int64_t attend_tokens_bytes(const hga_plan&, int, int, int, int) { return 64; }
 hipError_t launch_attend_tokens(const hga_plan&, const PoolView&, const TokensView&, const void*, int64_t, const int32_t*,
                                 int, void*, float*, void*, int64_t, hipStream_t) { return count(); }
