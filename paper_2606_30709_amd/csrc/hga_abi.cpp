@@ -204,6 +204,7 @@ hga_status hga_plan_create(const hga_params* params, hga_plan** plan) {
                     p.hf_pairs_chunk, p.hf_pairs_group);
     const std::vector<float> tg = phase_table(p.group, p.head_dim, p.rope_base, p.hf_pairs_group);
     const std::vector<float> tc = psi_table(p.chunk, p.group, p.head_dim, p.rope_base);
+    const std::vector<float> tp = phase_table(p.chunk, p.head_dim, p.rope_base, p.hf_pairs_chunk);
 
     int dev = -1;
     hipError_t e = hipGetDevice(&dev);
@@ -225,7 +226,7 @@ hga_status hga_plan_create(const hga_params* params, hga_plan** plan) {
     pl->max_lds = max_lds;
     pl->n_cu = n_cu;
     float* buf = nullptr;
-    const size_t bytes = (tc.size() + tg.size()) * sizeof(float);
+    const size_t bytes = (tc.size() + tg.size() + tp.size()) * sizeof(float);
     e = hipMalloc(&buf, bytes);
     if (e != hipSuccess) {
         delete pl;
@@ -234,6 +235,8 @@ hga_status hga_plan_create(const hga_params* params, hga_plan** plan) {
     e = hipMemcpy(buf, tg.data(), tg.size() * sizeof(float), hipMemcpyHostToDevice);
     if (e == hipSuccess)
         e = hipMemcpy(buf + tg.size(), tc.data(), tc.size() * sizeof(float), hipMemcpyHostToDevice);
+    if (e == hipSuccess)
+        e = hipMemcpy(buf + tg.size() + tc.size(), tp.data(), tp.size() * sizeof(float), hipMemcpyHostToDevice);
     if (e != hipSuccess) {
         (void)hipFree(buf);
         delete pl;
@@ -241,6 +244,7 @@ hga_status hga_plan_create(const hga_params* params, hga_plan** plan) {
     }
     pl->phase_group = buf;
     pl->phase_psi = buf + tg.size();
+    pl->phase_chunk = buf + tg.size() + tc.size();
     // the spread routing form's workspace: keys, then per-unit counters that
     // start at zero (each call leaves them at zero)
     void* ws = nullptr;

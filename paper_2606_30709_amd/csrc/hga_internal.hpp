@@ -15,6 +15,7 @@ struct hga_plan {
     int n_cu;             // compute units of the device
     float* phase_group;   // device [2][group][head_dim/2]: cos then sin of phi_p(o), span = group
     float* phase_psi;     // device [2][chunk/group][head_dim/2]: cos, sin of psi_g theta_p
+    float* phase_chunk;   // device [2][chunk][head_dim/2]: cos then sin of phi_p(o), span = chunk
     // routing workspace of the spread form (launches of a few units): keys
     // [kRouteSpreadUnits][kRouteSpreadCandidates], then one counter per unit
     // (zero between calls)

@@ -20,6 +20,17 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
     return o > x ? o : x;
 }
 
+__device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// The values of four codes of a block with exponent byte e.
+__device__ __forceinline__ void decode4(uint32_t codes, uint32_t e, float* x) {
+    const uint32_t lo = decode2<0>(codes, scale_of(e)), hi = decode2<1>(codes, scale_of(e));
+    x[0] = __uint_as_float(lo << 16);
+    x[1] = __uint_as_float(lo & 0xffff0000u);
+    x[2] = __uint_as_float(hi << 16);
+    x[3] = __uint_as_float(hi & 0xffff0000u);
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(PoolView pool, TokensView tok, const T* __restrict__ k,
                                                           int64_t k_stride, const T* __restrict__ v,
@@ -29,18 +40,18 @@ __global__ __launch_bounds__(kThreads) void append_kernel(PoolView pool, TokensV
     const int64_t item = static_cast<int64_t>(linear_block<kThreads>()) * (kThreads / kLanes) + threadIdx.x / kLanes;
     const int t = static_cast<int>(item / pool.n_kv), h = static_cast<int>(item % pool.n_kv);
     if (t >= tok.n_tokens) return;
-    int s, p;
-    if (!tok.at(t, s, p)) return;
-    const int id = tok.page_id(s, p / kPageRows);
-    if (!pool.has(id)) return;
     const int lane = threadIdx.x % kLanes;
     const bool key = lane < D / 8;
-    const int dim = lane % (D / 8) * 8, row = p % kPageRows;
-    float x[8];
+    const int dim = lane % (D / 8) * 8;
+    float x[8];  // fetched before the page is known
     load8((key ? k + t * k_stride : v + t * v_stride) + h * D + dim, x);
+    int s, p;
+    if (!tok.at(t, s, p)) return;
+    const int id = tok.page_id(s, p / kPageRows), row = p % kPageRows;
+    if (!pool.has(id)) return;
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    for (int j = 0; j < 8; ++j) m = max(m, bits_of(x[j]));
     const uint32_t e = block_scale(quad_max(m));
     const uint32_t codes = encode8(x, e);
     unsigned char* head = pool.page(id) + h * F::kBytes;
@@ -58,51 +69,80 @@ __global__ __launch_bounds__(kThreads) void append_kernel(PoolView pool, TokensV
     }
 }
 
-// Summary of every page that a token of the call fills (the token at its last row): the mean over the page's stored keys
-// turned to the page's middle, as the chunk summaries'.  A wavefront per (token, head).
+// A wavefront forms the summary of a page of one head: the mean over the stored keys turned to the page's middle, as the
+// chunk summaries are.  A lane holds four pairs of dimensions of every kAtOnce-th row.
 template <int D>
-__global__ __launch_bounds__(kThreads) void close_kernel(PoolView pool, TokensView tok,
-                                                         const float* __restrict__ phase_group,
-                                                         const float* __restrict__ phase_psi, int group, int hf_chunk) {
+__device__ __forceinline__ void summarise(const unsigned char* head, const float* __restrict__ phase, float* out) {
     using F = PageFormat<D>;
     constexpr int HALF = D / 2;
-    const int64_t item = static_cast<int64_t>(linear_block<kThreads>()) * (kThreads / 64) + threadIdx.x / 64;
-    const int t = static_cast<int>(item / pool.n_kv), h = static_cast<int>(item % pool.n_kv);
-    if (t >= tok.n_tokens) return;
-    int s, p;
-    if (!tok.at(t, s, p) || p % kPageRows != kPageRows - 1) return;
-    const int id = tok.page_id(s, p / kPageRows);
-    if (!pool.has(id)) return;
-    const unsigned char* head = pool.page(id) + h * F::kBytes;
-    const int lane = threadIdx.x & 63;
-    const int pair = lane % HALF;
-    if (lane >= HALF) return;
-    const int gpc = kPageRows / group;
-    const bool turn = pair >= hf_chunk;
-    float sa = 0.f, sb = 0.f;
-    for (int g = 0; g < gpc; ++g) {
-        float ga = 0.f, gb = 0.f;
-        for (int o = 0; o < group; ++o) {
-            const int row = g * group + o;
-            const int shift = 4 * (pair & 1);
-            auto value = [&](int dim) {
-                const uint32_t code = head[F::key_code(row, dim)] >> shift & 15u;
-                return __uint_as_float(decode2<0>(code, scale_of(head[F::key_scale(row, dim / 32)])) << 16);
-            };
-            const float a = value(pair), b = value(pair + HALF);
-            const float c = turn ? phase_group[o * HALF + pair] : 1.f;
-            const float sn = turn ? phase_group[(group + o) * HALF + pair] : 0.f;
-            ga += a * c - b * sn;
-            gb += a * sn + b * c;
+    constexpr int kRow = HALF / 4;      // lanes of a row
+    constexpr int kAtOnce = 64 / kRow;  // rows
+    constexpr int kBatch = 4;           // ... times this are fetched at once
+    const int lane = threadIdx.x & 63, dim = lane % kRow * 4, slot = lane / kRow;
+    float sa[4] = {}, sb[4] = {};
+#pragma unroll
+    for (int r0 = 0; r0 < kPageRows; r0 += kBatch * kAtOnce) {
+        uint32_t ca[kBatch], cb[kBatch], ea[kBatch], eb[kBatch];
+        float4 c[kBatch], sn[kBatch];
+#pragma unroll
+        for (int y = 0; y < kBatch; ++y) {
+            const int row = r0 + y * kAtOnce + slot;
+            ca[y] = *reinterpret_cast<const uint16_t*>(head + F::key_code(row, dim));
+            cb[y] = *reinterpret_cast<const uint16_t*>(head + F::key_code(row, dim + HALF));
+            ea[y] = head[F::key_scale(row, dim / 32)];
+            eb[y] = head[F::key_scale(row, (dim + HALF) / 32)];
+            c[y] = *reinterpret_cast<const float4*>(phase + row * HALF + dim);
+            sn[y] = *reinterpret_cast<const float4*>(phase + (kPageRows + row) * HALF + dim);
         }
-        const float c = turn ? phase_psi[g * HALF + pair] : 1.f;
-        const float sn = turn ? phase_psi[(gpc + g) * HALF + pair] : 0.f;
-        sa += ga * c - gb * sn;
-        sb += ga * sn + gb * c;
+#pragma unroll
+        for (int y = 0; y < kBatch; ++y) {
+            float a[4], b[4];
+            decode4(ca[y], ea[y], a);
+            decode4(cb[y], eb[y], b);
+            const float cy[4] = {c[y].x, c[y].y, c[y].z, c[y].w}, sy[4] = {sn[y].x, sn[y].y, sn[y].z, sn[y].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                sa[j] += a[j] * cy[j] - b[j] * sy[j];
+                sb[j] += a[j] * sy[j] + b[j] * cy[j];
+            }
+        }
     }
-    float* out = pool.sum + (static_cast<int64_t>(id) * pool.n_kv + h) * D;
-    out[pair] = sa * (1.f / kPageRows);
-    out[pair + HALF] = sb * (1.f / kPageRows);
+#pragma unroll
+    for (int m = kRow; m < 64; m *= 2)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            sa[j] += __shfl_xor(sa[j], m);
+            sb[j] += __shfl_xor(sb[j], m);
+        }
+    if (slot == 0) {
+        constexpr float f = 1.f / kPageRows;
+        *reinterpret_cast<float4*>(out + dim) = make_float4(sa[0] * f, sa[1] * f, sa[2] * f, sa[3] * f);
+        *reinterpret_cast<float4*>(out + dim + HALF) = make_float4(sb[0] * f, sb[1] * f, sb[2] * f, sb[3] * f);
+    }
+}
+
+// Summaries of the pages that the call's tokens fill (those at a page's last row), once all their rows are stored: a
+// workgroup looks at 64 tokens of a head (of a prompt one of them, of a decode step few but all of them at times), its
+// wavefronts take every kCloseWaves-th page.  Kept apart from the kernel before: with its registers that one, bound by
+// memory, had a third of the wavefronts it needs (23 K tokens of 8 heads of d64: 103 us together, 28 and 14 us apart).
+constexpr int kCloseWaves = 8;
+template <int D>
+__global__ __launch_bounds__(64 * kCloseWaves) void close_kernel(PoolView pool, TokensView tok,
+                                                                 const float* __restrict__ phase) {
+    using F = PageFormat<D>;
+    const int64_t block = linear_block<64 * kCloseWaves>();
+    const int h = static_cast<int>(block % pool.n_kv);
+    const int64_t t = block / pool.n_kv * 64 + (threadIdx.x & 63);
+    int s = 0, p = 0, id = -1;
+    if (t < tok.n_tokens && tok.at(static_cast<int>(t), s, p) && p % kPageRows == kPageRows - 1)
+        id = tok.page_id(s, p / kPageRows);
+    int n = 0;
+    for (uint64_t left = __builtin_amdgcn_ballot_w64(id >= 0 && pool.has(id)); left; left &= left - 1) {
+        if (n++ % kCloseWaves != static_cast<int>(threadIdx.x >> 6)) continue;
+        const int page = __builtin_amdgcn_readlane(id, static_cast<int>(__builtin_ctzll(left)));
+        summarise<D>(pool.page(page) + h * F::kBytes, phase,
+                     pool.sum + (static_cast<int64_t>(page) * pool.n_kv + h) * D);
+    }
 }
 
 template <typename T, int D>
@@ -206,13 +246,12 @@ template <typename T, int D>
 hipError_t append_t(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const void* k, int64_t k_stride,
                     const void* v, int64_t v_stride, hipStream_t stream) {
     constexpr int per = kThreads / (2 * D / 8);
-    const int64_t n = items(plan, tok);
-    append_kernel<T, D><<<grid_of((n + per - 1) / per, kThreads), kThreads, 0, stream>>>(
+    append_kernel<T, D><<<grid_of((items(plan, tok) + per - 1) / per, kThreads), kThreads, 0, stream>>>(
         pool, tok, static_cast<const T*>(k), k_stride, static_cast<const T*>(v), v_stride);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    close_kernel<D><<<grid_of((n + 3) / 4, kThreads), kThreads, 0, stream>>>(pool, tok, plan.phase_group, plan.phase_psi,
-                                                                            plan.p.group, plan.p.hf_pairs_chunk);
+    const int64_t blocks = (static_cast<int64_t>(tok.n_tokens) + 63) / 64 * plan.p.n_kv_heads;
+    close_kernel<D><<<grid_of(blocks, 64 * kCloseWaves), 64 * kCloseWaves, 0, stream>>>(pool, tok, plan.phase_chunk);
     return hipGetLastError();
 }
 
