@@ -595,6 +595,7 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
         }
     }
     if (c.tiles == 1 && units * c.splits < 2 * plan.n_cu) c.waves = 8;
+    if (c.tiles == 1 && c.splits == 1 && units >= 24 * plan.n_cu) c.waves = 1;
     return c;
 }
 
@@ -633,8 +634,10 @@ hipError_t launch_attend_tokens(const hga_plan& plan, const PoolView& pool, cons
         constexpr int D = decltype(dim)::value;
         constexpr int kTwo = sizeof(T) == 4 && D == 128 ? 1 : 2;
         const auto f = c.tokens > 1 ? (c.tiles == 2 ? run<T, D, kTwo, 4, true>
-                                       : c.waves == 8 ? run<T, D, 1, 8, true> : run<T, D, 1, 4, true>)
-                                    : c.waves == 8 ? run<T, D, 1, 8, false> : run<T, D, 1, 4, false>;
+                                       : c.waves == 8 ? run<T, D, 1, 8, true>
+                                       : c.waves == 1 ? run<T, D, 1, 1, true> : run<T, D, 1, 4, true>)
+                                    : c.waves == 8 ? run<T, D, 1, 8, false>
+                                    : c.waves == 1 ? run<T, D, 1, 1, false> : run<T, D, 1, 4, false>;
         return f(plan, pool, tok, a, q, q_stride, out, c.grid_units, stream);
     };
     const bool f32 = plan.p.dtype == HGA_F32;
