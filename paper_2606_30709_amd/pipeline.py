@@ -21,8 +21,14 @@ gather and the attention are either one call, ``hga_gather_attend``
 (``gather_mode="fused"``, the default: the attention stages the routed rows
 from the resident K/V and writes the routed buffers), or the two calls
 ``hga_gather_kv`` and ``hga_attend`` (``gather_mode="separate"``); the
-results are identical.  Both pipelines only allocate with torch and call the
-binding; all arithmetic runs in the HIP library.
+results are identical.
+
+``TokenPipeline``: single tokens of any sequences over a paged 4-bit cache
+(``pages.PagedCache``); one step appends a layer's rows, routes each token and
+attends it over its own pages.
+
+The pipelines only allocate with torch and call the binding; all arithmetic runs
+in the HIP library.
 """
 
 from __future__ import annotations
@@ -32,7 +38,8 @@ import torch
 
 from . import hga
 
-__all__ = ["PrefillPipeline", "BlockPrefillPipeline", "DecodePipeline", "to_device"]
+__all__ = ["PrefillPipeline", "BlockPrefillPipeline", "DecodePipeline", "TokenPipeline",
+           "to_device"]
 
 
 def to_device(arr: np.ndarray, dtype: str, device="cuda", pin=False) -> torch.Tensor:
@@ -517,3 +524,45 @@ class DecodeSequencePipeline:
         if self.cache is not None:
             return int(self.n_fetched.sum().item()) * 2 * w.group * row
         return int((self.group_idx >= 0).sum().item()) * 2 * w.group * row
+
+
+class TokenPipeline:
+    """One layer's attention of a batch of tokens over a ``PagedCache``: their
+    rows appended, each token routed to its own chunks (or, with ``routed``
+    false, given all of them) and attended.  Buffers are those of the largest
+    batch so far, so that a step of a size seen before allocates nothing (and
+    may be captured into a graph)."""
+
+    def __init__(self, cache, routed: bool = True):
+        self.cache, self.plan, self.routed = cache, cache.plan, routed
+        self._buf = {}
+
+    def _buffer(self, name, shape, dtype):
+        n = int(np.prod(shape))
+        t = self._buf.get(name)
+        if t is None or t.numel() < n:
+            t = self._buf[name] = torch.empty(max(n, 1), dtype=dtype, device=self.cache.pool.device)
+        return t[:n].view(shape)
+
+    def step(self, layer: int, batch: hga.TokenBatch, q, k, v, stream=None):
+        """q [n_tokens, n_q_heads, d], k and v [n_tokens, n_kv_heads, d]; returns
+        out (as q) and lse fp32 [n_tokens, n_q_heads], valid until the next
+        step."""
+        p, plan, pool = self.plan.params, self.plan, self.cache.pool
+        T = batch.n_tokens
+        out = self._buffer("out", (T, p.n_q_heads, p.head_dim), plan.torch_dtype)
+        lse = self._buffer("lse", (T, p.n_q_heads), torch.float32)
+        hga.hga_cache_append(plan, pool, layer, batch, k, v, stream=stream)
+        lists = None
+        if self.routed:
+            lists = self._buffer("lists", (T, p.n_kv_heads, hga.hga_token_list_size(plan)),
+                                 torch.int32)
+            nbytes = hga.hga_route_tokens_workspace(plan, batch)
+            hga.hga_route_tokens(plan, pool, layer, batch, q, lists,
+                                 workspace=self._buffer("route", (nbytes,), torch.uint8)
+                                 if nbytes else None, stream=stream)
+        nbytes = hga.hga_attend_tokens_workspace(plan, batch, lists)
+        hga.hga_attend_tokens(plan, pool, layer, batch, q, out, lse=lse, chunk_list=lists,
+                              workspace=self._buffer("attend", (nbytes,), torch.uint8)
+                              if nbytes else None, stream=stream)
+        return out, lse

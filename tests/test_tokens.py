@@ -485,3 +485,122 @@ def test_refusals(hga):
             make()
     torch.cuda.synchronize()
     assert (sc.pool.pages == 3).all()
+
+
+# ---------------------------------------------------- the operators together ---
+
+class _Twin:
+    """A PagedCache served token by token beside plain copies of what was
+    appended (as stored), attended in 64 bits."""
+
+    def __init__(self, hga, dtype, d, kv, ratio, routed, layers=2, topk=3, n_cold=6):
+        from paper_2606_30709_amd.pages import PagedCache
+        from paper_2606_30709_amd.pipeline import TokenPipeline
+        self.hga, self.dtype, self.d, self.kv, self.hq, self.routed = hga, dtype, d, kv, kv * ratio, routed
+        self.plan = hga.Plan(batch=1, n_q_heads=self.hq, n_kv_heads=kv, head_dim=d, keep_first=1, keep_last=1,
+                             topk_chunks=topk, topk_groups=4, dtype=hga.F32 if dtype == "f32" else hga.BF16)
+        self.cache = PagedCache(self.plan, 90, 4, 20, n_layers=layers, n_cold=n_cold)
+        self.pipe = TokenPipeline(self.cache, routed)
+        self.layers = layers
+        self.kept = [[[np.zeros((2, 0, kv, d))] for _ in range(layers)] for _ in range(4)]
+        self.rng = np.random.default_rng(3)
+        self.topk = topk
+
+    def rand(self, *s):
+        return torch.from_numpy(self.rng.standard_normal(s).astype(np.float32)).to(U.DT[self.dtype]).cuda()
+
+    def serve(self, seqs, counts, check=True):
+        batch = self.cache.append(seqs, counts)
+        T, hga = batch.n_tokens, self.hga
+        seq, pos = (x.cpu().numpy().astype(np.int64) for x in (batch.tok_seq, batch.tok_pos))
+        table = self.cache.page_table.cpu().numpy()
+        assert np.array_equal(table, self.cache.book.table)
+        results = []
+        for layer in range(self.layers):
+            q, k, v = self.rand(T, self.hq, self.d), self.rand(T, self.kv, self.d), self.rand(T, self.kv, self.d)
+            out, lse = self.pipe.step(layer, batch, q, k, v)
+            results.append((out.clone(), lse.clone()))
+            rows = [U.values(*U.quantise(f64(x))) for x in (k, v)]
+            for s in set(seq.tolist()):
+                self.kept[s][layer][0] = np.concatenate((self.kept[s][layer][0], np.stack([r[seq == s] for r in rows])), 1)
+            if not check:
+                continue
+            # pages rebuilt from what was appended
+            ids = self.cache.pool.n_pages + self.cache.pool.n_cold
+            kp, vp = np.zeros((2, ids, self.kv, PAGE, self.d))
+            for s in range(4):
+                x = self.kept[s][layer][0]
+                for c in range(-(-x.shape[1] // PAGE)):
+                    part = x[:, c * PAGE:(c + 1) * PAGE].transpose(0, 2, 1, 3)
+                    if table[s, c] >= 0:
+                        kp[table[s, c], :, :part.shape[2]], vp[table[s, c], :, :part.shape[2]] = part
+            lists = None
+            if self.routed:
+                sums = U.summary(kp, self.d, 10000.0, self.plan.params.hf_pairs_chunk)
+                n_list = hga.hga_token_list_size(self.plan)
+                lists = U.route(f64(q), sums, table, seq, pos, self.kv, 1, 1, self.topk, n_list, ids)
+                got = self.pipe._buffer("lists", (T, self.kv, n_list), torch.int32).cpu().numpy()
+                assert np.array_equal(got, lists)
+            ref, rlse, mag, reach, count = U.attend(f64(q), kp, vp, table, seq, pos, self.kv, lists, ids)
+            tol, ltol = U.attend_tolerance(self.dtype, self.d, ref, mag, reach, count)
+            assert (np.abs(f64(out) - ref) <= tol).all() and (np.abs(f64(lse) - rlse) <= ltol).all()
+        return results
+
+
+@pytest.mark.parametrize("dtype,d,kv,ratio,routed", [("bf16", 128, 2, 4, True), ("f32", 64, 2, 1, True),
+                                                     ("bf16", 64, 3, 2, False)])
+def test_serving_a_batch_of_sequences(hga, dtype, d, kv, ratio, routed):
+    """Prompts, single tokens, forks, drafts taken back, pages dropped, moved to
+    the cold tier and back, and moved together."""
+    t = _Twin(hga, dtype, d, kv, ratio, routed)
+    cache = t.cache
+    t.serve([2, 0], [300, 450])
+    t.serve([0, 2], [1, 1])
+    cache.fork(0, 1)
+    t.kept[1] = [[x[0].copy()] for x in t.kept[0]]
+    t.serve([1, 0, 2], [1, 1, 70])
+    cache.truncate(0, 400)
+    t.kept[0] = [[x[0][:, :400]] for x in t.kept[0]]
+    t.serve([0, 1], [3, 2])
+    assert cache.to_cold(1, 1, 6) == 5
+    t.serve([2, 1, 0], [1, 1, 200])
+    cache.drop(2, 1, 3)
+    cache.release(0)
+    t.kept[0] = [[x[0][:, :0]] for x in t.kept[0]]
+    t.serve([1, 2], [60, 1])
+    assert cache.compact() > 0
+    t.serve([2, 3, 1], [1, 130, 1])
+    assert cache.to_device(1, 0, 6) == 5
+    t.serve([1, 2, 3], [1, 1, 1])
+
+
+def test_moved_pages_give_the_same_bits(hga):
+    """Where pages lie changes nothing: compaction, the cold tier, a fork."""
+    t = _Twin(hga, "bf16", 128, 2, 4, True, n_cold=12)
+    cache = t.cache
+    t.serve([0, 1, 3], [333, 100, 700], check=False)
+    cache.release(1)
+    cache.fork(0, 2)
+
+    def look(s):
+        n = cache.length(s)
+        one = lambda x: torch.tensor([x], dtype=torch.int32).cuda()  # noqa: E731
+        batch = hga.TokenBatch(one(s), one(n - 1), cache.page_table)
+        g = torch.Generator().manual_seed(1)
+        q = torch.randn(1, t.hq, t.d, generator=g).bfloat16().cuda()
+        out = []
+        for layer in range(t.layers):
+            lists = torch.zeros(1, t.kv, hga.hga_token_list_size(t.plan), dtype=torch.int32, device="cuda")
+            hga.hga_route_tokens(t.plan, cache.pool, layer, batch, q, lists)
+            for ls in (lists, None):
+                o, l = torch.empty_like(q), torch.empty(1, t.hq, device="cuda")
+                hga.hga_attend_tokens(t.plan, cache.pool, layer, batch, q, o, lse=l, chunk_list=ls)
+                out += [o, l]
+        return out
+
+    first = look(0), look(3)
+    assert _same(first[0], look(2))
+    for change in (lambda: cache.to_cold(3, 0, 10), lambda: cache.compact(), lambda: cache.to_cold(0, 2, 4),
+                   lambda: cache.to_device(3, 1, 9), lambda: cache.compact()):
+        change()
+        assert _same(first[0], look(0)) and _same(first[1], look(3)) and _same(first[0], look(2))
