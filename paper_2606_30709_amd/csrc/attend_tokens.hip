@@ -297,14 +297,14 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared>)) vo
     float(*s_m)[16 * kTiles] = reinterpret_cast<float(*)[16 * kTiles]>(smem + kWaves * 16 * kTiles * (D + 4));
     float(*s_l)[16 * kTiles] = s_m + kWaves;
     const int n_units = kShared ? a.units[0] : tok.n_tokens;
-    const int64_t block = linear_block<kThreads>();
+    const uint32_t block = linear_block<kThreads>();
     // splits in the outer order: short histories have none of the later ones, and a split as the inner one would be an XCD
-    const int64_t row = static_cast<int64_t>(grid_units) * pool.n_kv;
+    const uint32_t row = static_cast<uint32_t>(grid_units) * pool.n_kv;
     const int split = static_cast<int>(block / row);
-    const int h = static_cast<int>(block % pool.n_kv);
+    const auto [unit0, h] = token_head(block % row, pool.n_kv);
     if (split >= a.splits) return;
-    for (int64_t unit = block % row / pool.n_kv; unit < n_units; unit += grid_units) {
-    const int t = kShared ? a.units[1 + unit] : static_cast<int>(unit);
+    for (int unit = unit0; unit < n_units; unit += grid_units) {
+    const int t = kShared ? a.units[1 + unit] : unit;
     const int n_tok = kShared ? a.units[2 + unit] - t : 1;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, g = lane >> 4;
     const int columns = n_tok * a.ratio;

@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kThreads) void route_block_kernel(PoolView pool, To
     __shared__ ChooseLds lds;
     __shared__ double s_q[D];
     const int64_t unit = linear_block<kThreads>();
-    const int t = static_cast<int>(unit / pool.n_kv), h = static_cast<int>(unit % pool.n_kv);
+    const auto [t, h] = token_head(static_cast<uint32_t>(unit), pool.n_kv);
     if (t >= tok.n_tokens) return;
     const int tid = threadIdx.x, sub = tid % kLanes;
     int32_t* out = list + unit * a.n_list;
@@ -342,15 +342,15 @@ __global__ __launch_bounds__(256) void score_slices_kernel(PoolView pool, Tokens
                                                            const T* __restrict__ q, int64_t q_stride,
                                                            uint64_t* __restrict__ ws) {
     __shared__ double s_q[D];
-    const int64_t block = linear_block<256>();
-    const int64_t unit = block / slices;
-    const int t = static_cast<int>(unit / pool.n_kv), h = static_cast<int>(unit % pool.n_kv);
+    const uint32_t block = linear_block<256>();
+    const int64_t unit = block / static_cast<uint32_t>(slices);
+    const auto [t, h] = token_head(static_cast<uint32_t>(unit), pool.n_kv);
     if (t >= tok.n_tokens) return;
     int s, p;
     if (!tok.at(t, s, p)) return;
     int lo, hi;
     middle(a, p / kPageRows, lo, hi);
-    const int n = hi - lo, i0 = static_cast<int>(block % slices) * kSlice;
+    const int n = hi - lo, i0 = static_cast<int>(block % static_cast<uint32_t>(slices)) * kSlice;
     if (i0 >= n) return;
     const int tid = threadIdx.x, sub = tid % kLanes;
     constexpr int kGroups = 256 / kLanes, kRows = kSlice / kGroups;
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(PoolView pool, TokensV
                                                           const uint64_t* __restrict__ ws, int32_t* __restrict__ list) {
     __shared__ ChooseLds lds;
     const int64_t unit = linear_block<kThreads>();
-    const int t = static_cast<int>(unit / pool.n_kv);
+    const int t = token_head(static_cast<uint32_t>(unit), pool.n_kv).t;
     if (t >= tok.n_tokens) return;
     int32_t* out = list + unit * a.n_list;
     int s, p;
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(256) void route_wave_kernel(PoolView pool, TokensVi
     __shared__ uint64_t s_k[4][64 * kLaneKeys];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane % kLanes;
     const int64_t unit = static_cast<int64_t>(linear_block<256>()) * 4 + wave;
-    const int t = static_cast<int>(unit / pool.n_kv), h = static_cast<int>(unit % pool.n_kv);
+    const auto [t, h] = token_head(static_cast<uint32_t>(unit), pool.n_kv);
     if (t >= tok.n_tokens) return;
     int32_t* out = list + unit * a.n_list;
     int s, p;

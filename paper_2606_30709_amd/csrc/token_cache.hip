@@ -37,8 +37,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(PoolView pool, TokensV
                                                           int64_t v_stride) {
     using F = PageFormat<D>;
     constexpr int kLanes = 2 * D / 8;  // lanes of a (token, head): keys, then values
-    const int64_t item = static_cast<int64_t>(linear_block<kThreads>()) * (kThreads / kLanes) + threadIdx.x / kLanes;
-    const int t = static_cast<int>(item / pool.n_kv), h = static_cast<int>(item % pool.n_kv);
+    const uint32_t item = linear_block<kThreads>() * (kThreads / kLanes) + threadIdx.x / kLanes;
+    const auto [t, h] = token_head(item, pool.n_kv);
     if (t >= tok.n_tokens) return;
     const int lane = threadIdx.x % kLanes;
     const bool key = lane < D / 8;
@@ -124,15 +124,14 @@ __device__ __forceinline__ void summarise(const unsigned char* head, const float
 // Summaries of the pages that the call's tokens fill (those at a page's last row), once all their rows are stored: a
 // workgroup looks at 64 tokens of a head (of a prompt one of them, of a decode step few but all of them at times), its
 // wavefronts take every kCloseWaves-th page.  Kept apart from the kernel before: with its registers that one, bound by
-// memory, had a third of the wavefronts it needs (23 K tokens of 8 heads of d64: 103 us together, 28 and 14 us apart).
-constexpr int kCloseWaves = 8;
+// memory, had a third of the wavefronts it needs (23 K tokens of 8 heads of d64: 103 us together, 28 and 9 us apart).
+constexpr int kCloseWaves = 4;
 template <int D>
 __global__ __launch_bounds__(64 * kCloseWaves) void close_kernel(PoolView pool, TokensView tok,
                                                                  const float* __restrict__ phase) {
     using F = PageFormat<D>;
-    const int64_t block = linear_block<64 * kCloseWaves>();
-    const int h = static_cast<int>(block % pool.n_kv);
-    const int64_t t = block / pool.n_kv * 64 + (threadIdx.x & 63);
+    const auto [t64, h] = token_head(linear_block<64 * kCloseWaves>(), pool.n_kv);
+    const int64_t t = static_cast<int64_t>(t64) * 64 + (threadIdx.x & 63);
     int s = 0, p = 0, id = -1;
     if (t < tok.n_tokens && tok.at(static_cast<int>(t), s, p) && p % kPageRows == kPageRows - 1)
         id = tok.page_id(s, p / kPageRows);
@@ -150,8 +149,8 @@ __global__ __launch_bounds__(kThreads) void read_kernel(PoolView pool, TokensVie
                                                         T* __restrict__ v) {
     using F = PageFormat<D>;
     constexpr int kLanes = 2 * D / 8;
-    const int64_t item = static_cast<int64_t>(linear_block<kThreads>()) * (kThreads / kLanes) + threadIdx.x / kLanes;
-    const int t = static_cast<int>(item / pool.n_kv), h = static_cast<int>(item % pool.n_kv);
+    const uint32_t item = linear_block<kThreads>() * (kThreads / kLanes) + threadIdx.x / kLanes;
+    const auto [t, h] = token_head(item, pool.n_kv);
     if (t >= tok.n_tokens) return;
     const int lane = threadIdx.x % kLanes;
     const bool key = lane < D / 8;
@@ -180,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(PoolView pool, TokensVie
     b.w[1] = decode2<1>(codes, sc);
     b.w[2] = decode2<2>(codes, sc);
     b.w[3] = decode2<3>(codes, sc);
-    T* out = (key ? k : v) + item * D + dim;
+    T* out = (key ? k : v) + static_cast<int64_t>(item) * D + dim;
     if constexpr (sizeof(T) == 2) {
         store16(out, b);
     } else {

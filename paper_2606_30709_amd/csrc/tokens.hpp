@@ -85,6 +85,15 @@ struct TokensView {
     }
 };
 
+// Token and head of a call's unit (or item) number, below 2^31: a division of 32-bit words.
+struct TokenHead {
+    int t, h;
+};
+__host__ __device__ inline TokenHead token_head(uint32_t unit, int n_kv) {
+    const uint32_t t = unit / static_cast<uint32_t>(n_kv);
+    return TokenHead{static_cast<int>(t), static_cast<int>(unit - t * static_cast<uint32_t>(n_kv))};
+}
+
 // An entry of a token's list of chunks, as a page and how many of its rows the token at position p sees (0: none).
 // Entries may hold anything.
 struct SeenPage {

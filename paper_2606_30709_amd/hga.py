@@ -534,8 +534,8 @@ def _rows(t, name: str, plan: Plan, n_tokens: int, heads: int, device) -> int:
     d = plan.params.head_dim
     _expect(t, name, plan.torch_dtype, (n_tokens, heads, d), device, contiguous=False)
     row, head, one = t.stride()
-    _require(n_tokens == 0 or (one == 1 and (heads == 1 or head == d)),
-             f"{name}: a token's heads must be contiguous")
+    if n_tokens and (one != 1 or (heads > 1 and head != d)):
+        _require(False, f"{name}: a token's heads must be contiguous")
     # a single token's stride means nothing (and may be anything)
     return row if n_tokens > 1 else heads * d
 
@@ -543,16 +543,17 @@ def _rows(t, name: str, plan: Plan, n_tokens: int, heads: int, device) -> int:
 def _space(workspace, device):
     if workspace is None:
         return None, 0
-    _require(workspace.is_contiguous() and workspace.device == device,
-             f"workspace must be a contiguous tensor on {device}")
+    if not workspace.is_contiguous() or workspace.device != device:
+        _require(False, f"workspace must be a contiguous tensor on {device}")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _on(pool, stream):
     """The stream to launch on: given, or the current one of the pool's device,
     which must be the current device."""
-    _require(pool.index == torch.cuda.current_device(),
-             f"the pool is on {pool.device}, the current device is {torch.cuda.current_device()}")
+    if pool.index != torch.cuda.current_device():
+        _require(False, f"the pool is on {pool.device}, the current device is "
+                        f"{torch.cuda.current_device()}")
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(pool.index)
     return _stream(stream)
@@ -621,8 +622,8 @@ def _size(n: int) -> int:
 
 
 def _same_device(pool: Pool, batch: TokenBatch):
-    _require(pool.index == batch.index,
-             f"the batch is on {batch.device}, the pool on {pool.device}")
+    if pool.index != batch.index:
+        _require(False, f"the batch is on {batch.device}, the pool on {pool.device}")
 
 
 def hga_page_bytes(plan: Plan) -> int:
