@@ -11,7 +11,9 @@
 // keys with a running reference (the maximum, or up to 2^kSlack below it) and sum of each column, in log2 units.
 //
 // fp32 queries and weights enter the matrix instructions as three bf16 terms each (24 bits); the stored keys and values are
-// exact in bf16.
+// exact in bf16.  With up to four query heads the terms are columns of their own (kSpread): column 4 r + x holds term x of
+// head r, the scores of four columns are added up, and each multiplies its own term of the weight.  A third of the matrix
+// instructions and half the work of splitting: 1,325 tokens of 12 heads of d64 over 11 pages each 125 -> 105 us.
 //
 // A wavefront loads its next page while it works on one; the wavefronts of a workgroup take every kWaves-th page and are
 // joined in LDS.  Long histories of few units are cut into equal runs of pages, a workgroup each, whose partial results a
@@ -54,6 +56,27 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t* w) {
 }
 
 // A lane's share of a page's keys and of its values.
+// The term of a value that column m holds in the spread form: bits 0-7, 8-15 and 16-23 of the significand, counted from the
+// top, each exact in bf16; the fourth column of a head holds zeros.
+struct TermMask {
+    uint32_t hi, lo;
+};
+__device__ __forceinline__ TermMask term_mask(int m) {
+    const uint32_t cut[4] = {0u, 0xffff0000u, 0xffffff00u, 0xffffffffu};
+    const int x = m & 3;
+    return TermMask{x == 0 ? cut[1] : x == 1 ? cut[2] : cut[3], x == 0 ? cut[0] : x == 1 ? cut[1] : x == 2 ? cut[2] : cut[3]};
+}
+__device__ __forceinline__ float term_of(float x, const TermMask& k) {
+    return __uint_as_float(__float_as_uint(x) & k.hi) - __uint_as_float(__float_as_uint(x) & k.lo);
+}
+// Sum over a head's four columns (the lanes of a quad).
+__device__ __forceinline__ float quad_sum(float x) {
+    x += __uint_as_float(static_cast<uint32_t>(
+        __builtin_amdgcn_mov_dpp(static_cast<int>(__float_as_uint(x)), 0xB1, 0xf, 0xf, true)));
+    return x + __uint_as_float(static_cast<uint32_t>(
+                   __builtin_amdgcn_mov_dpp(static_cast<int>(__float_as_uint(x)), 0x4E, 0xf, 0xf, true)));
+}
+
 template <int D>
 struct Keys {
     uint32_t c[4][D / 32];
@@ -183,7 +206,7 @@ __device__ __forceinline__ void page_scores(const Keys<D>& k, const u32x4 (&qf)[
 // Its weights under the running reference, four keys of a tile as two words.
 template <int D, int kTerms, int kTiles>
 __device__ __forceinline__ void page_weights(const f32x4 (&sc)[kTiles][4], float scale, Acc<D, kTiles>& acc,
-                                             uint32_t (&w)[kTiles][4][2][kTerms]) {
+                                             uint32_t (&w)[kTiles][4][2][kTerms], const TermMask* mask = nullptr) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
         float top = sc[i][0][0];
@@ -209,8 +232,16 @@ __device__ __forceinline__ void page_weights(const f32x4 (&sc)[kTiles][4], float
                 pv[x] = __builtin_amdgcn_exp2f(fmaf(sc[i][tt][x], scale, -base));
                 acc.l[i] += pv[x];
             }
-            split2<kTerms>(pv[0], pv[1], w[i][tt][0]);
-            split2<kTerms>(pv[2], pv[3], w[i][tt][1]);
+            if (mask) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) pv[x] = term_of(pv[x], *mask);
+                // exact in bf16: the high halves
+                w[i][tt][0][0] = __builtin_amdgcn_perm(__float_as_uint(pv[1]), __float_as_uint(pv[0]), 0x07060302u);
+                w[i][tt][1][0] = __builtin_amdgcn_perm(__float_as_uint(pv[3]), __float_as_uint(pv[2]), 0x07060302u);
+            } else {
+                split2<kTerms>(pv[0], pv[1], w[i][tt][0]);
+                split2<kTerms>(pv[2], pv[3], w[i][tt][1]);
+            }
         }
     }
 }
@@ -278,17 +309,21 @@ __device__ __forceinline__ float natural_lse(float base, float l) {
 }
 
 // Wavefronts of a SIMD that the registers are kept to (one tile: as many as fit without spills).
-template <typename T, int D, int kTiles, bool kShared>
-constexpr int kResident = kTiles == 2 || (sizeof(T) == 4 && D == 128) ? 2 : kShared ? 2 : sizeof(T) == 2 && D == 64 ? 4 : 3;
+template <typename T, int D, int kTiles, bool kShared, bool kSpread>
+constexpr int kResident = kTiles == 2 || kShared || (sizeof(T) == 4 && D == 128 && !kSpread) ? 2
+                          : sizeof(T) == 2 && D == 64                                       ? 4
+                                                                                            : 3;
 
 // kShared: units of several tokens, from a.units, of which a workgroup may take more than one; else every token is a unit.
-template <typename T, int D, int kTiles, int kWaves, bool kShared>
-__global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared>)) void attend_tokens_kernel(PoolView pool, TokensView tok, AttendArgs a,
+// kSpread: fp32, at most four heads and one token a unit, terms as columns.
+template <typename T, int D, int kTiles, int kWaves, bool kShared, bool kSpread>
+__global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared, kSpread>)) void attend_tokens_kernel(PoolView pool, TokensView tok, AttendArgs a,
                                                                     const T* __restrict__ q, int64_t q_stride,
                                                                     T* __restrict__ out, int grid_units) {
     using F = PageFormat<D>;
     constexpr int kThreads = 64 * kWaves;
-    constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;
+    static_assert(!kSpread || (sizeof(T) == 4 && !kShared && kTiles == 1), "");
+    constexpr int kTerms = sizeof(T) == 4 && !kSpread ? 3 : 1;
     constexpr int DL = F::kLaneDims;
     constexpr int kSteps = D / 32;
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(D));  // log2(e) / sqrt(d)
@@ -310,12 +345,13 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared>)) vo
     const int columns = n_tok * a.ratio;
 
     // column 16 i + m: query head column % r of token t + column / r; zeros past the last
+    const TermMask terms = term_mask(m);
     int pos[kTiles];
     int s = 0, last = -1, first = INT32_MAX;  // the unit's sequence, its tokens' largest and smallest positions
     u32x4 qf[kTiles][kTerms][kSteps];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-        const int c = 16 * i + m;
+        const int c = kSpread ? m >> 2 : 16 * i + m;
         const bool real = c < columns;
         const int tc = t + (real ? c / a.ratio : 0);
         int sc = 0, pc = 0;
@@ -329,6 +365,9 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared>)) vo
         for (int kk = 0; kk < kSteps; ++kk) {
             float x[8] = {};
             if (real && in) load8(row + 8 * kk, x);
+            if constexpr (kSpread)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = term_of(x[e], terms);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 uint32_t w[kTerms];
@@ -397,6 +436,11 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared>)) vo
             const int c = __builtin_amdgcn_readlane(chunk, cur);
             f32x4 sc[kTiles][4];
             page_scores<D, kTerms, kTiles>(k, qf, sc);
+            if constexpr (kSpread)
+#pragma unroll
+                for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) sc[0][tt][x] = quad_sum(sc[0][tt][x]);
             load_keys<D>(r, m, g, k);
             if (kShared ? first < c * kPageRows + kPageRows - 1 : __builtin_amdgcn_readlane(mine.rows, cur) < kPageRows) {
                 // rows past a column's position are not seen; those behind the last stored one hold anything, whose
@@ -415,7 +459,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared>)) vo
                     }
             }
             uint32_t w[kTiles][4][2][kTerms];
-            page_weights<D, kTerms, kTiles>(sc, scale, acc, w);
+            page_weights<D, kTerms, kTiles>(sc, scale, acc, w, kSpread ? &terms : nullptr);
             page_values<D, kTerms, kTiles>(v, w, acc);
             load_values<D>(r, m, g, v);
             cur = next;
@@ -426,13 +470,18 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared>)) vo
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
         const float l = sum_groups(acc.l[i]);
+        const int c = kSpread ? m >> 2 : 16 * i + m;
+        const bool holds = !kSpread || (m & 3) == 0;
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
-            for (int j = 0; j < DL; ++j) s_o[wave][16 * i + m][(4 * g + x) * DL + j] = acc.o[i][j][x];
-        if (g == 0) {
-            s_m[wave][16 * i + m] = acc.m[i];
-            s_l[wave][16 * i + m] = l;
+            for (int j = 0; j < DL; ++j) {
+                const float y = kSpread ? quad_sum(acc.o[i][j][x]) : acc.o[i][j][x];
+                if (holds) s_o[wave][c][(4 * g + x) * DL + j] = y;
+            }
+        if (g == 0 && holds) {
+            s_m[wave][c] = acc.m[i];
+            s_l[wave][c] = l;
         }
     }
     __syncthreads();
@@ -526,7 +575,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(int n_rows, int heads, 
     if (a.lse && threadIdx.x == 0) a.lse[row] = natural_lse(ref, l);
 }
 
-template <typename T, int D, int kTiles, int kWaves, bool kShared>
+template <typename T, int D, int kTiles, int kWaves, bool kShared, bool kSpread = false>
 hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const AttendArgs& a, const void* q,
                int64_t q_stride, void* out, int grid_units, hipStream_t stream) {
     constexpr int kThreads = 64 * kWaves;
@@ -534,13 +583,13 @@ hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok
     if (lds > 65536) {
         static std::atomic<uint64_t> done{0};
         const hipError_t e = once_per_device(done, plan.device, [] {
-            return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_tokens_kernel<T, D, kTiles, kWaves, kShared>),
+            return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_tokens_kernel<T, D, kTiles, kWaves, kShared, kSpread>),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
         });
         if (e != hipSuccess) return e;
     }
     const int64_t n = static_cast<int64_t>(grid_units) * pool.n_kv * a.splits;
-    attend_tokens_kernel<T, D, kTiles, kWaves, kShared><<<grid_of(n, kThreads), kThreads, lds, stream>>>(
+    attend_tokens_kernel<T, D, kTiles, kWaves, kShared, kSpread><<<grid_of(n, kThreads), kThreads, lds, stream>>>(
         pool, tok, a, static_cast<const T*>(q), q_stride, static_cast<T*>(out), grid_units);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
@@ -633,7 +682,10 @@ hipError_t launch_attend_tokens(const hga_plan& plan, const PoolView& pool, cons
         using T = decltype(zero);
         constexpr int D = decltype(dim)::value;
         constexpr int kTwo = sizeof(T) == 4 && D == 128 ? 1 : 2;
-        const auto f = c.tokens > 1 ? (c.tiles == 2 ? run<T, D, kTwo, 4, true>
+        constexpr bool kF32 = sizeof(T) == 4;
+        const auto spread = c.waves == 8 ? run<T, D, 1, 8, false, kF32>
+                            : c.waves == 1 ? run<T, D, 1, 1, false, kF32> : run<T, D, 1, 4, false, kF32>;
+        const auto f = kF32 && a.ratio <= 4 && c.tokens == 1 ? spread : c.tokens > 1 ? (c.tiles == 2 ? run<T, D, kTwo, 4, true>
                                        : c.waves == 8 ? run<T, D, 1, 8, true>
                                        : c.waves == 1 ? run<T, D, 1, 1, true> : run<T, D, 1, 4, true>)
                                     : c.waves == 8 ? run<T, D, 1, 8, false>

@@ -31,7 +31,7 @@ def _same(a, b):
 
 
 SHAPES = [("bf16", 128, 4, 8), ("f32", 128, 1, 16), ("bf16", 64, 3, 3), ("f32", 64, 2, 1), ("bf16", 64, 1, 16),
-          ("bf16", 128, 5, 2), ("f32", 128, 2, 5)]
+          ("bf16", 128, 5, 2), ("f32", 128, 2, 5), ("f32", 128, 2, 4), ("f32", 64, 3, 3)]
 
 
 # ------------------------------------------------------------- the store ---
