@@ -183,6 +183,9 @@ def test_a_prompts_tokens_route_alone(hga):
     sc = Scene(hga, "bf16", 64, 2, 4, lens=(1500, 300), topk=4)
     seq, pos = [0] * 1500 + [1] * 300, list(range(1500)) + list(range(300))
     _route_check(sc, sc.batch(seq, pos), sc.random(1800, sc.hq, 64))
+    # of a longer history: more chunks than a wavefront has lanes
+    sc = Scene(hga, "f32", 64, 2, 1, lens=(12001,), topk=40, last=2)
+    _route_check(sc, sc.batch([0] * 1100, range(12001 - 1100, 12001)), sc.random(1100, sc.hq, 64))
 
 
 def test_equal_scores_go_to_the_lowest_chunk(hga):
@@ -211,17 +214,20 @@ def test_scores_an_fp32_sum_cannot_tell_apart(hga):
     _route_check(sc, sc.batch([0], [64 * 300 - 1]), torch.ones(1, 2, 128, device="cuda"))
 
 
-def test_absent_pages_and_odd_summaries(hga):
-    sc = Scene(hga, "bf16", 128, 2, 3, lens=(64 * 60, 64 * 20), topk=6, last=2)
+@pytest.mark.parametrize("pages,copies", [(60, 1), (60, 400), (130, 400), (700, 1), (700, 60)])
+def test_absent_pages_and_odd_summaries(hga, pages, copies):
+    """In every form: few tokens and many, short histories and long."""
+    sc = Scene(hga, "bf16", 128, 2, 3, lens=(64 * pages, 64 * 20), topk=6, last=2)
     sc.table[0, 5:20] = -1
-    sc.table[0, [0, 57, 59]] = [sc.n_ids, 2 ** 31 - 1, -2 ** 31]
+    sc.table[0, [0, pages - 3, pages - 1]] = [sc.n_ids, 2 ** 31 - 1, -2 ** 31]
     sc.table[1, 1:17] = -1
     sums = sc.pool.page_sum[0]
     for i, x in zip((25, 30, 33, 41), (float("nan"), float("inf"), -float("inf"), 3e38)):
         sums[int(sc.table[0, i])] = x
-    q = sc.random(3, sc.hq, 128)
+    q = sc.random(3 * copies, sc.hq, 128)
     q[2] = q[2].abs() + 0.1
-    _route_check(sc, sc.batch([0, 1, 0], [64 * 60 - 1, 64 * 20 - 1, 64 * 60 - 1]), q)
+    q[1::5] = 0   # scores all equal, but for those that are not numbers
+    _route_check(sc, sc.batch([0, 1, 0] * copies, [64 * pages - 1, 64 * 20 - 1, 64 * pages - 1] * copies), q)
 
 
 @pytest.mark.parametrize("tokens", [1, 2, 40])
