@@ -649,7 +649,8 @@ typedef struct {
 int64_t hga_page_bytes(const hga_plan* plan);
 
 /* Chunks a token's list holds at most: keep_first + window + topk_chunks + 1,
- * window = max(keep_last, force_prev).  Host only. */
+ * window = max(keep_last, force_prev); lists of more than 2^20 entries are
+ * HGA_EUNSUPPORTED.  Host only. */
 int32_t hga_token_list_size(const hga_plan* plan);
 
 /* Append tokens to the cache: the rows of every token that is not idle and

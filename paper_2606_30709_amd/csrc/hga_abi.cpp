@@ -166,7 +166,7 @@ constexpr int32_t kMaxCacheSlots = 8192;
 
 extern "C" {
 
-int32_t hga_version(void) { return (1 << 16) | 0; }
+int32_t hga_version(void) { return (1 << 16) | 1; }
 
 int32_t hga_visible_chunks(const hga_params* params, int32_t c, int32_t* chunks, int32_t cap) {
     HGA_TRY(validate_params(params));

@@ -87,15 +87,25 @@ hga_status view_tokens(const hga_plan* plan, const hga_tokens* tok, const hga::P
 }
 
 // Rows of n_heads * head_dim elements, `stride` elements from token to token.
-hga_status check_rows(const hga_plan* plan, const void* x, int64_t stride, int n_heads, const char* name) {
+hga_status check_rows(const hga_plan* plan, int n_tokens, const void* x, int64_t stride, int n_heads, const char* name) {
     HGA_TRY(check_tensor(x, name));
     const int64_t elt = plan->p.dtype == HGA_F32 ? 4 : 2;
     if (stride < static_cast<int64_t>(n_heads) * plan->p.head_dim)
         return fail(HGA_EINVAL, "%s: a token stride of %lld elements is below a row's %d", name,
                     static_cast<long long>(stride), n_heads * plan->p.head_dim);
-    if (stride > INT64_MAX / 4 / hga::kMaxSeqPages || stride * elt % 16 != 0)
+    // no address space holds rows that far apart
+    if (stride > (int64_t(1) << 46) / n_tokens)
+        return fail(HGA_EINVAL, "%s: %d rows %lld elements apart", name, n_tokens, static_cast<long long>(stride));
+    if (stride * elt % 16 != 0)
         return fail(HGA_EALIGN, "%s: a token stride of %lld elements is not a multiple of 16 bytes", name,
                     static_cast<long long>(stride));
+    return HGA_OK;
+}
+
+constexpr int32_t kMaxList = 1 << 20;
+
+hga_status check_list(int32_t n_list) {
+    if (n_list > kMaxList) return fail(HGA_EUNSUPPORTED, "n_list %d above %d is not supported", n_list, kMaxList);
     return HGA_OK;
 }
 
@@ -116,7 +126,7 @@ int64_t hga_page_bytes(const hga_plan* plan) {
 int32_t hga_token_list_size(const hga_plan* plan) {
     if (!plan) return fail(HGA_EINVAL, "plan is NULL");
     const int64_t n = list_size(plan);
-    if (n > INT32_MAX) return fail(HGA_EUNSUPPORTED, "lists of more than 2^31 - 1 chunks are not supported");
+    if (n > kMaxList) return fail(HGA_EUNSUPPORTED, "lists of more than %d chunks are not supported", kMaxList);
     return static_cast<int32_t>(n);
 }
 
@@ -128,8 +138,8 @@ hga_status hga_cache_append(const hga_plan* plan, const hga_pool* pool, int32_t 
     HGA_TRY(view_pool(plan, pool, layer, &pv));
     HGA_TRY(view_tokens(plan, tokens, pv, &tv));
     if (tv.n_tokens == 0) return HGA_OK;
-    HGA_TRY(check_rows(plan, k, k_stride, plan->p.n_kv_heads, "k"));
-    HGA_TRY(check_rows(plan, v, v_stride, plan->p.n_kv_heads, "v"));
+    HGA_TRY(check_rows(plan, tv.n_tokens, k, k_stride, plan->p.n_kv_heads, "k"));
+    HGA_TRY(check_rows(plan, tv.n_tokens, v, v_stride, plan->p.n_kv_heads, "v"));
     clear_stale_error();
     return launched(hga::launch_cache_append(*plan, pv, tv, k, k_stride, v, v_stride, static_cast<hipStream_t>(stream)),
                     "hga_cache_append launch");
@@ -164,12 +174,13 @@ hga_status hga_route_tokens(const hga_plan* plan, const hga_pool* pool, int32_t 
     hga::TokensView tv;
     HGA_TRY(view_pool(plan, pool, layer, &pv));
     HGA_TRY(view_tokens(plan, tokens, pv, &tv));
+    HGA_TRY(check_list(n_list));
     if (n_list < list_size(plan))
         return fail(HGA_EINVAL, "n_list %d is below the %lld chunks a token may list", n_list,
                     static_cast<long long>(list_size(plan)));
     HGA_TRY(check_workspace(workspace, workspace_bytes));
     if (tv.n_tokens == 0) return HGA_OK;
-    HGA_TRY(check_rows(plan, q, q_stride, plan->p.n_q_heads, "q"));
+    HGA_TRY(check_rows(plan, tv.n_tokens, q, q_stride, plan->p.n_q_heads, "q"));
     HGA_TRY(check_index(chunk_list, "chunk_list"));
     const int64_t need = hga::route_tokens_bytes(*plan, tv.n_tokens, tv.max_pages, true);
     if (workspace_bytes < need)
@@ -186,6 +197,7 @@ int64_t hga_attend_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int3
     if (!plan) return fail(HGA_EINVAL, "plan is NULL");
     HGA_TRY(check_counts(plan, n_tokens, n_seqs, max_pages));
     if (n_list < 0) return fail(HGA_EINVAL, "n_list must be >= 0");
+    HGA_TRY(check_list(n_list));
     return hga::attend_tokens_bytes(*plan, n_tokens, n_seqs, max_pages, n_list);
 }
 
@@ -197,11 +209,13 @@ hga_status hga_attend_tokens(const hga_plan* plan, const hga_pool* pool, int32_t
     hga::TokensView tv;
     HGA_TRY(view_pool(plan, pool, layer, &pv));
     HGA_TRY(view_tokens(plan, tokens, pv, &tv));
-    if (n_list < 0 || (chunk_list != nullptr) != (n_list > 0))
-        return fail(HGA_EINVAL, "chunk_list and n_list: a list of n_list >= 1 entries, or NULL and 0");
+    if (n_list < 0) return fail(HGA_EINVAL, "n_list must be >= 0");
+    HGA_TRY(check_list(n_list));
     HGA_TRY(check_workspace(workspace, workspace_bytes));
     if (tv.n_tokens == 0) return HGA_OK;
-    HGA_TRY(check_rows(plan, q, q_stride, plan->p.n_q_heads, "q"));
+    if ((chunk_list != nullptr) != (n_list > 0))
+        return fail(HGA_EINVAL, "chunk_list and n_list: a list of n_list >= 1 entries, or NULL and 0");
+    HGA_TRY(check_rows(plan, tv.n_tokens, q, q_stride, plan->p.n_q_heads, "q"));
     HGA_TRY(check_tensor(out, "out"));
     if (chunk_list) HGA_TRY(check_index(chunk_list, "chunk_list"));
     if (lse) HGA_TRY(check_index(lse, "lse"));

@@ -591,6 +591,7 @@ class Pool:
         self.pages, self.page_sum, self.cold = pages, page_sum, cold
         self.n_layers, self.n_pages, self.n_cold = n_layers, n_pages, n_cold
         self.device, self.index = pages.device, pages.device.index
+        self.heads = (p.n_kv_heads, p.head_dim)
         self.struct = HgaPool(pages.data_ptr(), None if cold is None else cold.data_ptr(),
                               page_sum.data_ptr(), n_layers, n_pages, n_cold)
 
@@ -621,8 +622,11 @@ def _size(n: int) -> int:
     return n
 
 
-def _same_device(pool: Pool, batch: TokenBatch):
-    if pool.index != batch.index:
+def _match(plan: Plan, pool: Pool, batch: TokenBatch | None = None):
+    if pool.heads != (plan.params.n_kv_heads, plan.params.head_dim):
+        _require(False, f"the pool's (KV heads, head_dim) are {pool.heads}, the plan's "
+                        f"{(plan.params.n_kv_heads, plan.params.head_dim)}")
+    if batch is not None and pool.index != batch.index:
         _require(False, f"the batch is on {batch.device}, the pool on {pool.device}")
 
 
@@ -639,7 +643,7 @@ def hga_token_list_size(plan: Plan) -> int:
 def hga_cache_append(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, k, v, stream=None):
     """Stores k, v [n_tokens, n_kv_heads, head_dim] (token rows may be strided)
     in the tokens' pages in 4 bits and summarises the pages they fill."""
-    _same_device(pool, batch)
+    _match(plan, pool, batch)
     kv, dev = plan.params.n_kv_heads, pool.device
     ks = _rows(k, "k", plan, batch.n_tokens, kv, dev)
     vs = _rows(v, "v", plan, batch.n_tokens, kv, dev)
@@ -652,7 +656,7 @@ def hga_cache_read(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, k_out,
                    stream=None):
     """The values that the tokens' stored rows stand for, into k_out, v_out
     [n_tokens, n_kv_heads, head_dim]."""
-    _same_device(pool, batch)
+    _match(plan, pool, batch)
     shape = (batch.n_tokens, plan.params.n_kv_heads, plan.params.head_dim)
     _expect(k_out, "k_out", plan.torch_dtype, shape, pool.device)
     _expect(v_out, "v_out", plan.torch_dtype, shape, pool.device)
@@ -672,7 +676,7 @@ def hga_route_tokens(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, q, c
     """Each token's chunks into chunk_list int32 [n_tokens, n_kv_heads, n_list]
     (ascending, -1 behind); q [n_tokens, n_q_heads, head_dim], rows may be
     strided."""
-    _same_device(pool, batch)
+    _match(plan, pool, batch)
     qs = _rows(q, "q", plan, batch.n_tokens, plan.params.n_q_heads, pool.device)
     _expect(chunk_list, "chunk_list", torch.int32,
             (batch.n_tokens, plan.params.n_kv_heads, chunk_list.shape[-1]), pool.device)
@@ -694,7 +698,7 @@ def hga_attend_tokens(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, q, 
     sequence's) up to its own position.  q, out [n_tokens, n_q_heads, head_dim]
     (q's rows may be strided); lse fp32 [n_tokens, n_q_heads] or None;
     workspace: a device tensor, or None."""
-    _same_device(pool, batch)
+    _match(plan, pool, batch)
     p = plan.params
     qs = _rows(q, "q", plan, batch.n_tokens, p.n_q_heads, pool.device)
     _expect(out, "out", plan.torch_dtype, (batch.n_tokens, p.n_q_heads, p.head_dim), pool.device)
@@ -714,7 +718,8 @@ def hga_attend_tokens(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, q, 
 def hga_copy_pages(plan: Plan, pool: Pool, src, dst, stream=None):
     """Copies page src[i] over page dst[i] (int32 [n], on the GPU) in every
     layer, summaries included."""
-    _expect(src, "src", torch.int32, (None,), pool.device)
-    _expect(dst, "dst", torch.int32, (src.shape[0],), pool.device)
+    _match(plan, pool)
+    _expect(src, "src", torch.int32, (src.numel(),), pool.device)
+    _expect(dst, "dst", torch.int32, (src.numel(),), pool.device)
     _check(library().hga_copy_pages(plan.handle, ctypes.byref(pool.struct), _ptr(src), _ptr(dst),
                                     src.shape[0], _on(pool, stream)))

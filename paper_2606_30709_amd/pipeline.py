@@ -544,15 +544,15 @@ class TokenPipeline:
             t = self._buf[name] = torch.empty(max(n, 1), dtype=dtype, device=self.cache.pool.device)
         return t[:n].view(shape)
 
-    def step(self, layer: int, batch: hga.TokenBatch, q, k, v, stream=None):
+    def step(self, layer: int, batch: hga.TokenBatch, q, k, v):
         """q [n_tokens, n_q_heads, d], k and v [n_tokens, n_kv_heads, d]; returns
         out (as q) and lse fp32 [n_tokens, n_q_heads], valid until the next
-        step."""
+        step.  Runs on the current stream."""
         p, plan, pool = self.plan.params, self.plan, self.cache.pool
         T = batch.n_tokens
         out = self._buffer("out", (T, p.n_q_heads, p.head_dim), plan.torch_dtype)
         lse = self._buffer("lse", (T, p.n_q_heads), torch.float32)
-        hga.hga_cache_append(plan, pool, layer, batch, k, v, stream=stream)
+        hga.hga_cache_append(plan, pool, layer, batch, k, v)
         lists = None
         if self.routed:
             lists = self._buffer("lists", (T, p.n_kv_heads, hga.hga_token_list_size(plan)),
@@ -560,9 +560,9 @@ class TokenPipeline:
             nbytes = hga.hga_route_tokens_workspace(plan, batch)
             hga.hga_route_tokens(plan, pool, layer, batch, q, lists,
                                  workspace=self._buffer("route", (nbytes,), torch.uint8)
-                                 if nbytes else None, stream=stream)
+                                 if nbytes else None)
         nbytes = hga.hga_attend_tokens_workspace(plan, batch, lists)
         hga.hga_attend_tokens(plan, pool, layer, batch, q, out, lse=lse, chunk_list=lists,
                               workspace=self._buffer("attend", (nbytes,), torch.uint8)
-                              if nbytes else None, stream=stream)
+                              if nbytes else None)
         return out, lse

@@ -479,7 +479,10 @@ def test_refusals(hga):
     for s, t in ((i32, i32[:2]), (i32.long(), i32), (i32.cpu(), i32.cpu())):
         with pytest.raises(hga.HgaError):
             copy(s, t)
-    for make in (lambda: hga.Pool(sc.plan, pages=sc.pool.pages[..., :-1].contiguous()),
+    other = hga.Plan(batch=1, n_q_heads=2, n_kv_heads=2, head_dim=128, topk_chunks=1, topk_groups=1)
+    for make in (lambda: hga.hga_copy_pages(other, sc.pool, i32, i32),
+                 lambda: hga.hga_cache_append(other, sc.pool, 0, b, q[..., :1], q[..., :1]),
+                 lambda: hga.Pool(sc.plan, pages=sc.pool.pages[..., :-1].contiguous()),
                  lambda: hga.Pool(sc.plan, pages=sc.pool.pages.cpu()),
                  lambda: hga.Pool(sc.plan, pages=sc.pool.pages, cold=sc.pool.cold.clone()),
                  lambda: hga.Pool(sc.plan, pages=sc.pool.pages, page_sum=sc.pool.page_sum[:, :1].contiguous()),
@@ -560,6 +563,8 @@ def test_serving_a_batch_of_sequences(hga, dtype, d, kv, ratio, routed):
     the cold tier and back, and moved together."""
     t = _Twin(hga, dtype, d, kv, ratio, routed)
     cache = t.cache
+    t.serve([], [])
+    t.serve([1], [0])
     t.serve([2, 0], [300, 450])
     t.serve([0, 2], [1, 1])
     cache.fork(0, 1)

@@ -145,7 +145,7 @@ static void refusals() {
     EXPECT(hga_route_tokens_workspace(&plan, 1, (1 << 18) + 1) == HGA_EUNSUPPORTED);
     EXPECT(append(-1) == HGA_EINVAL && append(2) == HGA_EINVAL && append(0, nullptr) == HGA_EINVAL && append(0, at(4)) == HGA_EALIGN);
     EXPECT(append(0, buf, 127) == HGA_EINVAL && append(0, buf, 132) == HGA_EALIGN && append(0, buf, 128, 0) == HGA_EINVAL);
-    EXPECT(append(0, buf, -128) == HGA_EINVAL && append(0, buf, INT64_MAX & ~int64_t(15)) == HGA_EALIGN);
+    EXPECT(append(0, buf, -128) == HGA_EINVAL && append(0, buf, INT64_MAX & ~int64_t(15)) == HGA_EINVAL);
     EXPECT(hga_cache_read(&plan, &pool, 0, &tok, nullptr, buf, nullptr) == HGA_EINVAL);
     EXPECT(hga_cache_read(&plan, &pool, 0, &tok, buf, at(8), nullptr) == HGA_EALIGN);
     EXPECT(route(5) == HGA_EINVAL && route(6, nullptr) == HGA_EINVAL && route(6, buf, 255) == HGA_EINVAL && route(6, buf, 260) == HGA_EALIGN);
@@ -159,6 +159,12 @@ static void refusals() {
     EXPECT(attend(nullptr, 0, buf, at(8), 8) == HGA_EALIGN && attend(nullptr, 0, buf, nullptr, 8) == HGA_EINVAL);
     EXPECT(attend(nullptr, 0, buf, nullptr, 0, reinterpret_cast<float*>(buf + 1)) == HGA_EALIGN);
     EXPECT(attend(reinterpret_cast<int32_t*>(buf + 1), 2) == HGA_EALIGN);
+    EXPECT(route((1 << 20) + 1) == HGA_EUNSUPPORTED && attend(ids, (1 << 20) + 1) == HGA_EUNSUPPORTED);
+    EXPECT(hga_attend_tokens_workspace(&plan, 1, 1, 1, (1 << 20) + 1) == HGA_EUNSUPPORTED);
+    EXPECT(append(0, buf, (int64_t(1) << 46) / 3 / 8 * 8 + 8) == HGA_EINVAL);
+    plan.p.keep_first = INT_MAX;
+    EXPECT(hga_token_list_size(&plan) == HGA_EUNSUPPORTED && route(1 << 20) == HGA_EINVAL);
+    plan.p.keep_first = 1;
     EXPECT(copy(-1) == HGA_EINVAL && copy(1, nullptr) == HGA_EINVAL && copy(1, at(1)) == HGA_EALIGN && copy(1 << 28) == HGA_EUNSUPPORTED);
     for (int n : {-1, 1}) {
         hga_tokens bad = tok;

@@ -13,7 +13,7 @@ DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 def quantise(x):
     """x [..., d] -> codes uint8 [..., d], scale bytes uint8 [..., d/32]."""
-    b = np.asarray(x, np.float64).reshape(*x.shape[:-1], -1, 32)
+    b = np.asarray(x, np.float64).reshape(*x.shape[:-1], x.shape[-1] // 32, 32)
     fin = np.isfinite(b).all(-1)
     amax = np.where(fin, np.abs(np.where(np.isfinite(b), b, 0)).max(-1), 0)
     s = np.full(amax.shape, -125)
