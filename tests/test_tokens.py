@@ -315,6 +315,48 @@ def test_one_token_after_a_long_history(hga, dtype):
         sc.check_attend(q, sc.attend(batch, q, workspace=max(part, 16)))
 
 
+@pytest.mark.parametrize("dtype,d,kv,ratio,new", [("bf16", 128, 1, 4, 45), ("f32", 64, 2, 3, 40), ("f32", 128, 1, 6, 30),
+                                                  ("bf16", 64, 2, 16, 7)])
+def test_a_draft_after_a_long_history(hga, dtype, d, kv, ratio, new):
+    """Tokens that share their pages, the history cut into runs, some of its
+    pages absent, some cold; with every size of workspace."""
+    n = 64 * 90 + 11
+    sc = Scene(hga, dtype, d, kv, ratio, lens=(n, 100, 64 * 70), cold=20, seed=7)
+    sc.table[0, 20:31] = -1
+    sc.table[2, [0, 69]] = sc.n_ids
+    runs = [(0, n - new, n), (1, 90, 100), (2, 64 * 70 - new, 64 * 70)]
+    seq = np.concatenate([[s] * (b - a) for s, a, b in runs])
+    pos = np.concatenate([np.arange(a, b) for _, a, b in runs])
+    batch = sc.batch(seq, pos)
+    q = sc.random(len(seq), sc.hq, d)
+    most = hga.hga_attend_tokens_workspace(sc.plan, batch)
+    assert most > 0
+    full = sc.attend(batch, q)
+    sc.check_attend(q, full)
+    assert _same(full, sc.attend(batch, q))
+    for nb in (16, 4 * len(seq) + 16, most // 2 // 16 * 16, most + 64):
+        sc.check_attend(q, sc.attend(batch, q, workspace=nb), tokens=slice(0, None, 7))
+
+
+@pytest.mark.parametrize("dtype,ratio", [("bf16", 2), ("f32", 2), ("f32", 5)])
+def test_thousands_of_units(hga, dtype, ratio):
+    """More units than the device holds wavefronts: a wavefront each."""
+    sc = Scene(hga, dtype, 64, 2, ratio, lens=(200, 65, 1, 400), seed=9)
+    sc.table = np.tile(sc.table, (800, 1))
+    lens = np.tile(sc.lens, 800)
+    some = np.r_[0:40, 3000:3100, -30:0]
+    # two tokens a sequence
+    seq = np.repeat(np.arange(3200), 2)
+    pos = np.stack((lens - 1, lens // 2), 1).reshape(-1)
+    batch = sc.batch(seq, pos)
+    q = sc.random(len(seq), sc.hq, 64)
+    sc.check_attend(q, sc.attend(batch, q), tokens=some)
+    sc.check_attend(q, sc.attend(batch, q, workspace=False), tokens=some)
+    # lists of their own, in any order
+    lists = torch.from_numpy(sc.rng.integers(-1, 8, (len(seq), 2, 5)).astype(np.int32)).cuda()
+    sc.check_attend(q, sc.attend(batch, q, lists), lists, tokens=some)
+
+
 def test_scores_far_apart_and_rows_that_are_not_numbers(hga):
     sc = Scene(hga, "bf16", 64, 2, 2, lens=(500, 500), seed=6)
     q = sc.random(2, 4, 64, scale=60.0)   # a weight of one, the rest far below
@@ -414,6 +456,44 @@ def test_other_streams_and_replayed_graphs(hga):
             st["batch"].tok_pos.add_(1)
     assert np.array_equal(a.stored(), b.stored())
     assert torch.equal(a.pool.page_sum, b.pool.page_sum)
+
+
+def test_replays_find_nothing_in_their_workspace(hga):
+    """A captured call over a split history, tokens sharing pages: replayed with
+    other positions and queries, its workspace filled with anything between."""
+    n = 64 * 80
+    sc = Scene(hga, "bf16", 128, 1, 4, lens=(n, n), seed=10)
+    seq = torch.tensor([0] * 9 + [1] * 5, dtype=torch.int32)
+    pos = torch.arange(14, dtype=torch.int32) + n - 40
+    batch = sc.batch(seq.numpy(), pos.numpy())
+    q, out = sc.random(14, 4, 128), torch.zeros(14, 4, 128, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(14, 4, device="cuda")
+    lists = torch.zeros(14, 1, hga.hga_token_list_size(sc.plan), dtype=torch.int32, device="cuda")
+    nb = hga.hga_attend_tokens_workspace(sc.plan, batch)
+    ws = torch.zeros(nb, dtype=torch.uint8, device="cuda")
+    rws = torch.zeros(max(hga.hga_route_tokens_workspace(sc.plan, batch), 16), dtype=torch.uint8, device="cuda")
+
+    def calls(out, lse, lists):
+        hga.hga_route_tokens(sc.plan, sc.pool, 0, batch, q, lists, workspace=rws)
+        hga.hga_attend_tokens(sc.plan, sc.pool, 0, batch, q, out, lse=lse, workspace=ws)
+
+    calls(out, lse, lists)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(out, lse, lists)
+    for i in range(5):
+        q.copy_(sc.random(14, 4, 128))
+        batch.tok_pos.add_(3)
+        batch.tok_seq.copy_(seq.roll(i))
+        ws.fill_(255 - i)
+        rws.random_()
+        graph.replay()
+        eager = torch.empty_like(out), torch.empty_like(lse), torch.empty_like(lists)
+        calls(*eager)
+        assert _same((out, lse), eager[:2]) and torch.equal(lists, eager[2])
+        sc.seq, sc.pos = batch.tok_seq.cpu().numpy(), batch.tok_pos.cpu().numpy()
+        sc.check_attend(q, (out, lse))
 
 
 def test_no_tokens_and_empty_tables(hga):

@@ -235,13 +235,15 @@ class Scene:
                               workspace=ws, stream=stream)
         return out, lse
 
-    def check_attend(self, q, got, lists=None):
+    def check_attend(self, q, got, lists=None, tokens=slice(None)):
+        """Of the given tokens of a call (all)."""
         out, lse = got
         k, v = self.k_v()
-        ln = None if lists is None else lists.cpu().numpy()
-        ref, rlse, mag, reach, count = attend(f64(q), k, v, self.table, self.seq, self.pos, self.kv, ln, self.n_ids)
+        ln = None if lists is None else lists.cpu().numpy()[tokens]
+        ref, rlse, mag, reach, count = attend(f64(q)[tokens], k, v, self.table, self.seq[tokens], self.pos[tokens],
+                                              self.kv, ln, self.n_ids)
         tol, ltol = attend_tolerance(self.dtype, self.d, ref, mag, reach, count)
-        o, l = f64(out), f64(lse)
+        o, l = f64(out)[tokens], f64(lse)[tokens]
         none = count == 0
         assert (o[none] == 0).all() and (l[none] == -np.inf).all()
         assert np.isfinite(o).all() and np.isfinite(l[~none]).all()
