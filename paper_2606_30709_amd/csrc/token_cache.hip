@@ -31,16 +31,12 @@ __device__ __forceinline__ void decode4(uint32_t codes, uint32_t e, float* x) {
     x[3] = __uint_as_float(hi & 0xffff0000u);
 }
 
+// Stores a lane's eight dimensions of a row of a (token, head): lanes 0 .. D/8 - 1 the keys', the next the values'.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void append_kernel(PoolView pool, TokensView tok, const T* __restrict__ k,
-                                                          int64_t k_stride, const T* __restrict__ v,
-                                                          int64_t v_stride) {
+__device__ __forceinline__ void store_piece(const PoolView& pool, const TokensView& tok, int t, int h, int lane,
+                                            const T* __restrict__ k, int64_t k_stride, const T* __restrict__ v,
+                                            int64_t v_stride) {
     using F = PageFormat<D>;
-    constexpr int kLanes = 2 * D / 8;  // lanes of a (token, head): keys, then values
-    const uint32_t item = linear_block<kThreads>() * (kThreads / kLanes) + threadIdx.x / kLanes;
-    const auto [t, h] = token_head(item, pool.n_kv);
-    if (t >= tok.n_tokens) return;
-    const int lane = threadIdx.x % kLanes;
     const bool key = lane < D / 8;
     const int dim = lane % (D / 8) * 8;
     float x[8];  // fetched before the page is known
@@ -67,6 +63,15 @@ __global__ __launch_bounds__(kThreads) void append_kernel(PoolView pool, TokensV
         }
         if (dim % 32 == 0) head[F::value_scale(row, dim / 32)] = static_cast<unsigned char>(e);
     }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void append_kernel(PoolView pool, TokensView tok, const T* __restrict__ k,
+                                                          int64_t k_stride, const T* __restrict__ v,
+                                                          int64_t v_stride) {
+    constexpr int kLanes = 2 * D / 8;  // lanes of a (token, head): keys, then values
+    const auto [t, h] = token_head(linear_block<kThreads>() * (kThreads / kLanes) + threadIdx.x / kLanes, pool.n_kv);
+    if (t < tok.n_tokens) store_piece<T, D>(pool, tok, t, h, threadIdx.x % kLanes, k, k_stride, v, v_stride);
 }
 
 // A wavefront forms the summary of a page of one head: the mean over the stored keys turned to the page's middle, as the
@@ -126,22 +131,46 @@ __device__ __forceinline__ void summarise(const unsigned char* head, const float
 // wavefronts take every kCloseWaves-th page.  Kept apart from the kernel before: with its registers that one, bound by
 // memory, had a third of the wavefronts it needs (23 K tokens of 8 heads of d64: 103 us together, 28 and 9 us apart).
 constexpr int kCloseWaves = 4;
-template <int D>
-__global__ __launch_bounds__(64 * kCloseWaves) void close_kernel(PoolView pool, TokensView tok,
-                                                                 const float* __restrict__ phase) {
+template <int D, int kOf>
+__device__ __forceinline__ void close_pages(const PoolView& pool, const TokensView& tok, int64_t t0, int h,
+                                            const float* __restrict__ phase) {
     using F = PageFormat<D>;
-    const auto [t64, h] = token_head(linear_block<64 * kCloseWaves>(), pool.n_kv);
-    const int64_t t = static_cast<int64_t>(t64) * 64 + (threadIdx.x & 63);
+    const int64_t t = t0 + (threadIdx.x & 63);
     int s = 0, p = 0, id = -1;
     if (t < tok.n_tokens && tok.at(static_cast<int>(t), s, p) && p % kPageRows == kPageRows - 1)
         id = tok.page_id(s, p / kPageRows);
     int n = 0;
     for (uint64_t left = __builtin_amdgcn_ballot_w64(id >= 0 && pool.has(id)); left; left &= left - 1) {
-        if (n++ % kCloseWaves != static_cast<int>(threadIdx.x >> 6)) continue;
+        if (n++ % kOf != static_cast<int>(threadIdx.x >> 6)) continue;
         const int page = __builtin_amdgcn_readlane(id, static_cast<int>(__builtin_ctzll(left)));
         summarise<D>(pool.page(page) + h * F::kBytes, phase,
                      pool.sum + (static_cast<int64_t>(page) * pool.n_kv + h) * D);
     }
+}
+template <int D>
+__global__ __launch_bounds__(64 * kCloseWaves) void close_kernel(PoolView pool, TokensView tok,
+                                                                 const float* __restrict__ phase) {
+    const auto [t64, h] = token_head(linear_block<64 * kCloseWaves>(), pool.n_kv);
+    close_pages<D, kCloseWaves>(pool, tok, static_cast<int64_t>(t64) * 64, h, phase);
+}
+
+// Both in one launch, for calls of at most kFewTokens tokens: a workgroup stores every row of a head, and so knows them
+// stored when it looks for the pages they fill.  4 heads of d128, a call in a graph (and on the host): 1 token 4.5 us (6.4)
+// against 5.8 (9.1) in two launches, 32 tokens 5.5 against 6.1, 64 tokens 7.0 against 6.2.
+constexpr int kFewTokens = 32, kFewWaves = 8;
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kFewWaves) void append_few_kernel(PoolView pool, TokensView tok,
+                                                                    const T* __restrict__ k, int64_t k_stride,
+                                                                    const T* __restrict__ v, int64_t v_stride,
+                                                                    const float* __restrict__ phase) {
+    constexpr int kLanes = 2 * D / 8, kAtOnce = 64 * kFewWaves / kLanes;
+    const int h = static_cast<int>(linear_block<64 * kFewWaves>());
+    if (h >= pool.n_kv) return;
+#pragma unroll 4
+    for (int t = threadIdx.x / kLanes; t < tok.n_tokens; t += kAtOnce)
+        store_piece<T, D>(pool, tok, t, h, threadIdx.x % kLanes, k, k_stride, v, v_stride);
+    __syncthreads();
+    for (int t = 0; t < tok.n_tokens; t += 64) close_pages<D, kFewWaves>(pool, tok, t, h, phase);
 }
 
 template <typename T, int D>
@@ -244,6 +273,11 @@ int64_t items(const hga_plan& plan, const TokensView& tok) {
 template <typename T, int D>
 hipError_t append_t(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const void* k, int64_t k_stride,
                     const void* v, int64_t v_stride, hipStream_t stream) {
+    if (tok.n_tokens <= kFewTokens) {
+        append_few_kernel<T, D><<<grid_of(plan.p.n_kv_heads, 64 * kFewWaves), 64 * kFewWaves, 0, stream>>>(
+            pool, tok, static_cast<const T*>(k), k_stride, static_cast<const T*>(v), v_stride, plan.phase_chunk);
+        return hipGetLastError();
+    }
     constexpr int per = kThreads / (2 * D / 8);
     append_kernel<T, D><<<grid_of((items(plan, tok) + per - 1) / per, kThreads), kThreads, 0, stream>>>(
         pool, tok, static_cast<const T*>(k), k_stride, static_cast<const T*>(v), v_stride);
