@@ -119,8 +119,8 @@ def test_tokens_one_by_one_are_the_prompt(hga, dtype, d, kv):
     assert torch.equal(one.pool.page_sum, all_.pool.page_sum)
     # a rejected draft: positions appended again hold what was appended last
     k2, v2 = one.random(100, kv, d), one.random(100, kv, d)
-    for a, b in ((50, 100), (100, 150)):
-        hga.hga_cache_append(one.plan, one.pool, 0, one.batch([0] * 50, range(a, b)), k2[a - 50:b - 50],
+    for a, b in ((50, 75), (75, 100), (100, 102), (102, 150)):
+        hga.hga_cache_append(one.plan, one.pool, 0, one.batch([0] * (b - a), range(a, b)), k2[a - 50:b - 50],
                              v2[a - 50:b - 50])
     hga.hga_cache_append(all_.plan, all_.pool, 0, all_.batch([0] * 150, range(n)), torch.cat((k[:50], k2)),
                          torch.cat((v[:50], v2)))
