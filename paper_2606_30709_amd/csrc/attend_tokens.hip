@@ -22,8 +22,7 @@
 #include <type_traits>
 
 #include "hga_device.hpp"
-#include "hga_internal.hpp"
-#include "tokens.hpp"
+#include "tokens_internal.hpp"
 
 namespace hga {
 namespace {

@@ -226,6 +226,7 @@ hga_status hga_plan_create(const hga_params* params, hga_plan** plan) {
     pl->max_lds = max_lds;
     pl->n_cu = n_cu;
     float* buf = nullptr;
+    // the page's table behind the two that the plan names (hga::phase_chunk)
     const size_t bytes = (tc.size() + tg.size() + tp.size()) * sizeof(float);
     e = hipMalloc(&buf, bytes);
     if (e != hipSuccess) {
@@ -244,7 +245,6 @@ hga_status hga_plan_create(const hga_params* params, hga_plan** plan) {
     }
     pl->phase_group = buf;
     pl->phase_psi = buf + tg.size();
-    pl->phase_chunk = buf + tg.size() + tc.size();
     // the spread routing form's workspace: keys, then per-unit counters that
     // start at zero (each call leaves them at zero)
     void* ws = nullptr;

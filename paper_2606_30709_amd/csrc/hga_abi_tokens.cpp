@@ -5,8 +5,7 @@
 
 #include "abi_common.hpp"
 #include "hga.h"
-#include "hga_internal.hpp"
-#include "tokens.hpp"
+#include "tokens_internal.hpp"
 
 using namespace hga::abi;
 

@@ -15,7 +15,6 @@ struct hga_plan {
     int n_cu;             // compute units of the device
     float* phase_group;   // device [2][group][head_dim/2]: cos then sin of phi_p(o), span = group
     float* phase_psi;     // device [2][chunk/group][head_dim/2]: cos, sin of psi_g theta_p
-    float* phase_chunk;   // device [2][chunk][head_dim/2]: cos then sin of phi_p(o), span = chunk
     // routing workspace of the spread form (launches of a few units): keys
     // [kRouteSpreadUnits][kRouteSpreadCandidates], then one counter per unit
     // (zero between calls)
@@ -197,35 +196,5 @@ hipError_t launch_gather_attend(const hga_plan& plan, const void* q_rot, int q_c
                                 int64_t res_tokens, const int32_t* group_idx, void* k_routed,
                                 void* v_routed, void* out, float* lse, hipEvent_t start,
                                 hipEvent_t stop, hipStream_t stream, bool block_major = false);
-
-// The paged 4-bit cache (tokens.hpp): appending tokens (and summarising the
-// pages they fill), reading rows back, copying pages.  cold: the device
-// address of the pool's cold tier.
-struct PoolView;
-struct TokensView;
-hipError_t launch_cache_append(const hga_plan& plan, const PoolView& pool, const TokensView& tok,
-                               const void* k, int64_t k_stride, const void* v, int64_t v_stride,
-                               hipStream_t stream);
-hipError_t launch_cache_read(const hga_plan& plan, const PoolView& pool, const TokensView& tok,
-                             void* k, void* v, hipStream_t stream);
-int64_t copy_pages_workgroups(const hga_plan& plan);  // of one page in one layer
-hipError_t launch_copy_pages(const hga_plan& plan, const hga_pool& pool, void* cold,
-                             const int32_t* src, const int32_t* dst, int n, hipStream_t stream);
-
-// Routing of single tokens to pages, and the workspace bytes it makes use of
-// (or cannot do without).
-int64_t route_tokens_bytes(const hga_plan& plan, int n_tokens, int max_pages, bool must);
-hipError_t launch_route_tokens(const hga_plan& plan, const PoolView& pool, const TokensView& tok,
-                               const void* q, int64_t q_stride, int32_t* list, int n_list, void* ws,
-                               int64_t ws_bytes, hipStream_t stream);
-
-// Attention of single tokens over listed pages (list NULL: all), and the
-// bytes its workspace may take.
-int64_t attend_tokens_bytes(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages,
-                            int n_list);
-hipError_t launch_attend_tokens(const hga_plan& plan, const PoolView& pool, const TokensView& tok,
-                                const void* q, int64_t q_stride, const int32_t* list, int n_list,
-                                void* out, float* lse, void* ws, int64_t ws_bytes,
-                                hipStream_t stream);
 
 }  // namespace hga

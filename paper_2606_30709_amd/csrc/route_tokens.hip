@@ -15,8 +15,7 @@
 #include <algorithm>
 
 #include "hga_device.hpp"
-#include "hga_internal.hpp"
-#include "tokens.hpp"
+#include "tokens_internal.hpp"
 
 namespace hga {
 namespace {

@@ -4,8 +4,7 @@
 // the block's largest magnitude among themselves, and a lane's eight codes are one word of the page.  Both are bound by
 // their bytes (a token of 4 heads of d128: 2 KiB of bf16 in, 544 bytes out).
 #include "hga_device.hpp"
-#include "hga_internal.hpp"
-#include "tokens.hpp"
+#include "tokens_internal.hpp"
 
 namespace hga {
 namespace {
@@ -275,7 +274,7 @@ hipError_t append_t(const hga_plan& plan, const PoolView& pool, const TokensView
                     const void* v, int64_t v_stride, hipStream_t stream) {
     if (tok.n_tokens <= kFewTokens) {
         append_few_kernel<T, D><<<grid_of(plan.p.n_kv_heads, 64 * kFewWaves), 64 * kFewWaves, 0, stream>>>(
-            pool, tok, static_cast<const T*>(k), k_stride, static_cast<const T*>(v), v_stride, plan.phase_chunk);
+            pool, tok, static_cast<const T*>(k), k_stride, static_cast<const T*>(v), v_stride, phase_chunk(plan));
         return hipGetLastError();
     }
     constexpr int per = kThreads / (2 * D / 8);
@@ -284,7 +283,7 @@ hipError_t append_t(const hga_plan& plan, const PoolView& pool, const TokensView
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t blocks = (static_cast<int64_t>(tok.n_tokens) + 63) / 64 * plan.p.n_kv_heads;
-    close_kernel<D><<<grid_of(blocks, 64 * kCloseWaves), 64 * kCloseWaves, 0, stream>>>(pool, tok, plan.phase_chunk);
+    close_kernel<D><<<grid_of(blocks, 64 * kCloseWaves), 64 * kCloseWaves, 0, stream>>>(pool, tok, phase_chunk(plan));
     return hipGetLastError();
 }
 
