@@ -89,14 +89,17 @@ struct Values {
 
 // One head's part of a page as a buffer: no address arithmetic per lane but a fixed offset, and an empty buffer's loads
 // touch no memory, so that the loop below needs no branch around its last loads.
+// Codes are loaded past the caches (kNt): histories of a decode step are read once (32 of them up to 32K tokens: 67 us
+// cached, 60 so), and prompts, whose units share pages, take the same time either way.
+constexpr int kNt = 2;
 template <int D>
 __device__ __forceinline__ void load_codes(buf_rsrc r, uint32_t offset, uint32_t (&w)[D / 32]) {
     if constexpr (D == 128) {
-        const vec16 x = buf_load16(r, offset);
+        const vec16 x = __builtin_bit_cast(vec16, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, kNt));
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = x.w[i];
     } else {
-        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 0));
+        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, kNt));
         w[0] = x.x;
         w[1] = x.y;
     }

@@ -234,7 +234,7 @@ hga_status hga_copy_pages(const hga_plan* plan, const hga_pool* pool, const int3
     HGA_TRY(check_index(dst, "dst"));
     void* cold = nullptr;
     HGA_TRY(map_cold(pool, &cold));
-    if (static_cast<int64_t>(n) * pool->n_layers > kMaxUnits / hga::copy_pages_workgroups(*plan))
+    if (static_cast<int64_t>(n) * pool->n_layers > kMaxUnits)
         return fail(HGA_EUNSUPPORTED, "%d pages of %d layers in one call are not supported", n, pool->n_layers);
     clear_stale_error();
     return launched(hga::launch_copy_pages(*plan, *pool, cold, src, dst, n, static_cast<hipStream_t>(stream)),

@@ -149,12 +149,27 @@ __device__ __forceinline__ uint32_t encode8(const float* x, uint32_t e) {
     return r;
 }
 
-// Eight consecutive elements of a row, 16-byte loads.
+// 16 bytes read or written once: not kept in the caches.
+__device__ __forceinline__ vec16 load16_once(const void* p) {
+    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(vec16, __builtin_nontemporal_load(static_cast<const u32x4_t*>(p)));
+}
+__device__ __forceinline__ void store16_once(void* p, const vec16& v) {
+    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), static_cast<u32x4_t*>(p));
+}
+
+// Eight consecutive elements of a row, 16-byte loads; _once: of a row read once.
 __device__ __forceinline__ void load8(const float* p, float* x) {
     elem<float>::unpack(load16(p), x);
     elem<float>::unpack(load16(p + 4), x + 4);
 }
 __device__ __forceinline__ void load8(const bf16_t* p, float* x) { elem<bf16_t>::unpack(load16(p), x); }
+__device__ __forceinline__ void load8_once(const float* p, float* x) {
+    elem<float>::unpack(load16_once(p), x);
+    elem<float>::unpack(load16_once(p + 4), x + 4);
+}
+__device__ __forceinline__ void load8_once(const bf16_t* p, float* x) { elem<bf16_t>::unpack(load16_once(p), x); }
 
 #endif
 

@@ -20,7 +20,6 @@ hipError_t launch_cache_append(const hga_plan& plan, const PoolView& pool, const
                                hipStream_t stream);
 hipError_t launch_cache_read(const hga_plan& plan, const PoolView& pool, const TokensView& tok,
                              void* k, void* v, hipStream_t stream);
-int64_t copy_pages_workgroups(const hga_plan& plan);  // of one page in one layer
 hipError_t launch_copy_pages(const hga_plan& plan, const hga_pool& pool, void* cold,
                              const int32_t* src, const int32_t* dst, int n, hipStream_t stream);
 

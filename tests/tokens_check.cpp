@@ -30,7 +30,6 @@ static hipError_t count() {
 hipError_t launch_cache_append(const hga_plan&, const PoolView&, const TokensView&, const void*, int64_t, const void*,
                                int64_t, hipStream_t) { return count(); }
 hipError_t launch_cache_read(const hga_plan&, const PoolView&, const TokensView&, void*, void*, hipStream_t) { return count(); }
-int64_t copy_pages_workgroups(const hga_plan&) { return 4; }
 hipError_t launch_copy_pages(const hga_plan&, const hga_pool&, void*, const int32_t*, const int32_t*, int, hipStream_t) { return count(); }
 int64_t route_tokens_bytes(const hga_plan&, int, int max_pages, bool) { return max_pages > 100 ? 64 : 0; }
 hipError_t launch_route_tokens(const hga_plan&, const PoolView&, const TokensView&, const void*, int64_t, int32_t*, int,
@@ -165,7 +164,7 @@ static void refusals() {
     plan.p.keep_first = INT_MAX;
     EXPECT(hga_token_list_size(&plan) == HGA_EUNSUPPORTED && route(1 << 20) == HGA_EINVAL);
     plan.p.keep_first = 1;
-    EXPECT(copy(-1) == HGA_EINVAL && copy(1, nullptr) == HGA_EINVAL && copy(1, at(1)) == HGA_EALIGN && copy(1 << 28) == HGA_EUNSUPPORTED);
+    EXPECT(copy(-1) == HGA_EINVAL && copy(1, nullptr) == HGA_EINVAL && copy(1, at(1)) == HGA_EALIGN && copy((1 << 29) + 1) == HGA_EUNSUPPORTED);
     for (int n : {-1, 1}) {
         hga_tokens bad = tok;
         if (n < 0) bad.n_tokens = n; else bad.tok_pos = nullptr;
