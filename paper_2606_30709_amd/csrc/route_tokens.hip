@@ -135,10 +135,12 @@ __device__ __forceinline__ int block_scan(int x, int* s_w, int& total) {  // exc
     return before;
 }
 
-// The border of a selection: keys above `key` (under `mask`) are taken, of those equal to it the first `ties`.
+// The border of a selection: keys above `key` (under `mask`) are taken, of those equal to it the first `ties` (all: there
+// are no more of them).
 struct Border {
     uint64_t key, mask;
     int ties;
+    bool all;
 };
 
 struct ChooseLds {
@@ -150,12 +152,13 @@ struct ChooseLds {
     int bin, above, n_cand;
     uint64_t border;
     int ties;
+    bool all;
 };
 
 // By counting, from the most significant byte down: any keys.
 __device__ __forceinline__ Border border_by_bytes(const uint64_t* keys, int n, int k, ChooseLds& s) {
     const int tid = threadIdx.x;
-    Border b{0, 0, k};
+    Border b{0, 0, k, false};
     for (int shift = 56; shift >= 0; shift -= 8) {
         if (tid < 256) s.hist[tid] = 0;
         __syncthreads();
@@ -172,7 +175,10 @@ __device__ __forceinline__ Border border_by_bytes(const uint64_t* keys, int n, i
         b.mask |= uint64_t(255) << shift;
         b.ties -= above;
         __syncthreads();
-        if (in == b.ties) break;  // all of the bin
+        if (in == b.ties) {  // all of the bin
+            b.all = true;
+            break;
+        }
     }
     return b;
 }
@@ -223,19 +229,21 @@ __device__ __forceinline__ Border find_border(const uint64_t* keys, int n, int k
     __syncthreads();
     if (tid < in) {
         const uint64_t v = s.cand[tid];
-        int rank = 0, equal = 1;  // keys before this one; equal ones up to it
+        int rank = 0, upto = 1, equal = 0;  // keys before this one; equal ones up to it, and in all
         for (int i = 0; i < in; ++i) {
-            const bool tie = s.cand[i] == v && s.cand_at[i] < s.cand_at[tid];
+            const bool same = s.cand[i] == v, tie = same && s.cand_at[i] < s.cand_at[tid];
             rank += s.cand[i] > v || tie;
-            equal += tie;
+            upto += tie;
+            equal += same;
         }
         if (rank == need - 1) {
             s.border = v;
-            s.ties = equal;
+            s.ties = upto;
+            s.all = upto == equal;
         }
     }
     __syncthreads();
-    return Border{s.border, ~uint64_t(0), s.ties};
+    return Border{s.border, ~uint64_t(0), s.ties, s.all};
 }
 
 // A unit's list from its keys[0..n) of middle chunks lo .. lo + n - 1.
@@ -259,34 +267,44 @@ __device__ __forceinline__ void choose(const PoolView& pool, const TokensView& t
         lds.hi[wave] = most;
     }
     block_scan(found, lds.scan, total);
-    Border b{0, 0, 0};
-    const bool some = total > a.topk;  // more candidates than are taken
-    if (some) {
+    Border b{0, 0, 0, true};
+    if (total > a.topk) {  // more candidates than are taken
         for (int w = 0; w < kWaves; ++w) {
             least = lds.lo[w] < least ? lds.lo[w] : least;
             most = lds.hi[w] > most ? lds.hi[w] : most;
         }
         b = find_border(keys, n, a.topk, least, most, lds);
     }
-    // thread i takes a run of chunks; their ranks from two scans, of the ties and of the chosen
+    // thread i takes a run of chunks; their ranks from a scan of the chosen, and one of the ties where some are left out
     const int per = own / kThreads + 1, c0 = min(tid * per, own + 1), c1 = min(c0 + per, own + 1);
     const auto key = [&](int c) { return keys[c - lo]; };
-    int ties = 0;
-    if (some)
+    int ties0 = 0;
+    if (!b.all) {
+        int ties = 0;
         for (int c = max(c0, lo); c < min(c1, lo + n); ++c) ties += key(c) != 0 && (key(c) & b.mask) == b.key;
-    const int ties0 = some ? block_scan(ties, lds.scan, total) : 0;
+        ties0 = block_scan(ties, lds.scan, total);
+    }
     const auto pick = [&](int c, int& tie) {
         if (c < lo || c >= lo + n) return pool.has(tok.page_id(s, c));
         const uint64_t v = key(c) & b.mask;
         if (key(c) == 0 || v < b.key) return false;
-        return !some || v != b.key || tie++ < b.ties;
+        return b.all || v != b.key || tie++ < b.ties;
     };
-    int count = 0, tie = ties0;
-    for (int c = c0; c < c1; ++c) count += pick(c, tie);
-    int rank = block_scan(count, lds.scan, total);
-    tie = ties0;
-    for (int c = c0; c < c1; ++c)
-        if (pick(c, tie) && rank < a.n_list) out[rank++] = c;
+    if (per <= 64) {  // a run's choices fit a word: made once
+        uint64_t picked = 0;
+        for (int c = c0; c < c1; ++c)
+            if (pick(c, ties0)) picked |= uint64_t(1) << (c - c0);
+        int rank = block_scan(__popcll(picked), lds.scan, total);
+        for (; picked; picked &= picked - 1, ++rank)
+            if (rank < a.n_list) out[rank] = c0 + static_cast<int>(__builtin_ctzll(picked));
+    } else {
+        int count = 0, tie = ties0;
+        for (int c = c0; c < c1; ++c) count += pick(c, tie);
+        int rank = block_scan(count, lds.scan, total);
+        tie = ties0;
+        for (int c = c0; c < c1; ++c)
+            if (pick(c, tie) && rank < a.n_list) out[rank++] = c;
+    }
     for (int i = total + tid; i < a.n_list; i += kThreads) out[i] = -1;
 }
 

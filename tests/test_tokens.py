@@ -230,10 +230,10 @@ def test_absent_pages_and_odd_summaries(hga, pages, copies):
     _route_check(sc, sc.batch([0, 1, 0] * copies, [64 * pages - 1, 64 * 20 - 1, 64 * pages - 1] * copies), q)
 
 
-@pytest.mark.parametrize("tokens", [1, 2, 40])
-def test_histories_of_a_million_tokens(hga, tokens):
+@pytest.mark.parametrize("tokens,pages", [(1, 16400), (2, 16400), (40, 16400), (1, 70001)])
+def test_histories_of_a_million_tokens(hga, tokens, pages):
     """16,400 and more chunks (over pages that recur): the workspace form."""
-    n = 16400 + tokens
+    n = pages + tokens
     sc = Scene(hga, "bf16", 64, 2, 2, lens=(64 * 500,), topk=9, max_pages=n)
     sc.table[0] = sc.table[0, sc.rng.integers(0, 500, n)]
     sc.sums = None
