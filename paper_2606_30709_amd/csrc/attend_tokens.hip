@@ -628,8 +628,8 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
     }
     const int64_t units = static_cast<int64_t>((n_tokens + c.tokens - 1) / c.tokens) * plan.p.n_kv_heads;
     c.run = static_cast<int>(entries);
-    // workgroups that the device holds at once or a few more (decode of 32 histories up to 32K, 4 heads of d128: 68 us with 4
-    // a CU, 72-78 with 2, 3, 6 or 8; 512 tokens of a 16K prompt in two tiles: 171 us with 2, 186 with 4)
+    // workgroups that the device holds at once or a few more (decode of 32 histories up to 32K, 4 heads of d128: 60 us with 4
+    // a CU, 66-70 with 2, 3 or 6; 512 tokens of a 16K prompt in two tiles: 171 us with 2, 186 with 4)
     const int64_t want = (c.tiles == 2 ? 2 : 4) * static_cast<int64_t>(plan.n_cu);
     if (entries > 64 && units < want) {
         const int64_t run = std::max<int64_t>(16, (units * entries + want - 1) / want);
