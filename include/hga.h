@@ -658,11 +658,11 @@ int32_t hga_token_list_size(const hga_plan* plan);
  * position is among them gets its summary.
  *   k, v  [n_tokens][n_kv_heads][head_dim] plan dtype (strided, see above); K
  *         rotated at its position
- * The tokens of one sequence stand next to each other in ascending order of
- * position (other sequences' before and after), no position twice, and no two
- * sequences of the call write to one page (hga_copy_pages before appending to
- * a shared one).  A position may be appended again later (a rejected draft):
- * pages hold no state besides their rows. */
+ * The tokens stand in any order, but none twice, and no two sequences of the
+ * call write to one page (hga_copy_pages before appending to a shared one).  A
+ * summary is that of the page's 64 rows once the call's are stored.  A position
+ * may be appended again later (a rejected draft): pages hold no state besides
+ * their rows. */
 hga_status hga_cache_append(const hga_plan* plan, const hga_pool* pool, int32_t layer,
                             const hga_tokens* tokens, const void* k, int64_t k_stride,
                             const void* v, int64_t v_stride, void* stream);

@@ -117,6 +117,12 @@ def test_tokens_one_by_one_are_the_prompt(hga, dtype, d, kv):
         hga.hga_cache_append(one.plan, one.pool, 0, one.batch([0], [a]), k[a:a + 1], v[a:a + 1])
     assert np.array_equal(one.stored(), all_.stored())
     assert torch.equal(one.pool.page_sum, all_.pool.page_sum)
+    # ... in any order
+    o = torch.from_numpy(one.rng.permutation(n))
+    mixed = Scene(hga, dtype, d, kv, 2, lens=(n,), seed=3)
+    hga.hga_cache_append(mixed.plan, mixed.pool, 0, mixed.batch([0] * n, o.numpy()), k[o.cuda()], v[o.cuda()])
+    assert np.array_equal(mixed.stored(), all_.stored())
+    assert torch.equal(mixed.pool.page_sum, all_.pool.page_sum)
     # a rejected draft: positions appended again hold what was appended last
     k2, v2 = one.random(100, kv, d), one.random(100, kv, d)
     for a, b in ((50, 75), (75, 100), (100, 102), (102, 150)):
