@@ -631,8 +631,20 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
     // workgroups that the device holds at once or a few more (decode of 32 histories up to 32K, 4 heads of d128: 60 us with 4
     // a CU, 66-70 with 2, 3 or 6; 512 tokens of a 16K prompt in two tiles: 171 us with 2, 186 with 4)
     const int64_t want = (c.tiles == 2 ? 2 : 4) * static_cast<int64_t>(plan.n_cu);
-    if (entries > 64 && units < want) {
-        const int64_t run = std::max<int64_t>(16, (units * entries + want - 1) / want);
+    // A history is split where the join costs less than the pages that a workgroup would take one after another: over 64
+    // pages, and from fewer where the units leave half of the device idle. 4 heads of d128, split and whole, in us: 1
+    // sequence of 20 pages 8.5 and 9.1, of 32 8.8 and 11.9, of 64 9.1 and 18.1; 16 of 20 10.6 and 10.1, of 32 11.2 and
+    // 12.8; 32 of 32 13.8 and 13.8, of 64 18.8 and 21.8. Tokens of one sequence in two tiles: 4 at 20 pages 16.2 and 20.1,
+    // 64 at 20 pages 20.8 and 20.6, at 32 22.0 and 24.5; 128 at 32 29.6 and 25.1, at 60 34.0 and 33.9.
+    const int64_t whole = 2 * units > plan.n_cu ? 64 : 16 + units / 8;
+    if (entries > whole && units < want) {
+        // A run is 16 pages or more where the device is filled: a part is written and read again. Below that it is the run
+        // that gives each compute unit a workgroup, of two tiles every other one, 4 pages at the least (1 sequence of 64
+        // pages: 9.1 us in runs of 4, 10.0 of 8, 11.4 of 16; 8 sequences: 12.3, 11.1, 12.4; 32 tokens in two tiles at 100
+        // pages: 26.1 in runs of 13, 23.0 of 16).
+        const int64_t fill = std::max<int64_t>(1, plan.n_cu / (units * c.tiles));
+        const int64_t least = std::clamp<int64_t>((entries + fill - 1) / fill, 4, 16);
+        const int64_t run = std::max(least, (units * entries + want - 1) / want);
         const int64_t counts = pad16(int64_t(n_tokens) * 4);
         const int64_t split_bytes = pad16(rows * plan.p.head_dim * 4) + pad16(rows * 8);
         const int64_t splits = std::min((entries + run - 1) / run, (ws_bytes - c.bytes - counts) / split_bytes);
@@ -645,7 +657,11 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
             c.bytes += counts + splits * split_bytes;
         }
     }
-    if (c.tiles == 1 && units * c.splits < 2 * plan.n_cu) c.waves = 8;
+    // A workgroup of 8 wavefronts where a compute unit has one workgroup only (1 sequence of 64 pages, whole: 17.4 us, 18.9
+    // with 4; 64 sequences of 31 listed pages: 15.1 and 15.7; at 400 units of 32 pages 27.4 and 23.4). One wavefront, which
+    // joins nothing, from 24 a compute unit on (16K units of 3 fp32 heads of d64: 130 us, 165 with 4; 6.4K units of bf16
+    // d128: 177 either way; at 1,600 units 58 and 51).
+    if (c.tiles == 1 && units * c.splits <= plan.n_cu) c.waves = 8;
     if (c.tiles == 1 && c.splits == 1 && units >= 24 * plan.n_cu) c.waves = 1;
     return c;
 }

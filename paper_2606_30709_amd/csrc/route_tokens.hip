@@ -509,9 +509,10 @@ __global__ __launch_bounds__(256) void route_wave_kernel(PoolView pool, TokensVi
 }
 
 // Few units of long histories take two kernels: where a workgroup a unit would leave most of the device idle for the
-// time that one takes over its summaries (128K tokens: 1 MiB at 512 bytes a chunk).
+// time that one takes over its summaries (128K tokens: 1 MiB at 512 bytes a chunk). 4 heads of d128, in two and in one: 1
+// token at 32K 9.3 and 8.6 us, at 128K 11.9 and 17.1; 16 sequences at 64K 13.8 and 13.9.
 bool few_and_long(const hga_plan& plan, int64_t units, int max_pages) {
-    return max_pages > kLdsPages || (max_pages >= 4 * kSlice && units * 4 <= plan.n_cu);
+    return max_pages > kLdsPages || (max_pages >= 8 * kSlice && units * 4 <= plan.n_cu);
 }
 
 template <typename T, int D>
@@ -527,8 +528,11 @@ hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok
         choose_kernel<<<grid_of(units, kThreads), kThreads, 0, stream>>>(pool, tok, a, ws, list);
         return hipGetLastError();
     }
-    if (tok.max_pages <= 64 * kLaneKeys && units >= 8 * plan.n_cu) {
-        // 64 chunks or fewer: a key a lane (4,096 tokens of 3 heads: 19.5 us with four, 16 with one)
+    // A wavefront a unit: up to 64 chunks, a key a lane, at any count (3 heads of d64 at 4K, 1 token: 4.9 us, 6.6 with a
+    // workgroup; 330 tokens: 5.7 and 12.5); up to four keys a lane where the units fill the device (1 token at 8K: 7.1 and
+    // 6.7 us, 330: 8.4 and 12.7; 256 tokens at 16K: 10.8 and 10.3, 400: 12.9 and 15.0).
+    if (tok.max_pages <= 64 || (tok.max_pages <= 64 * kLaneKeys && units >= 4 * plan.n_cu)) {
+        // a key a lane or four: 4,096 tokens of 3 heads at 4K 16 and 19.5 us
         const auto kernel = tok.max_pages <= 64 ? route_wave_kernel<T, D, 1> : route_wave_kernel<T, D, kLaneKeys>;
         kernel<<<grid_of((units + 3) / 4, 256), 256, 0, stream>>>(pool, tok, a, qt, q_stride, list);
         return hipGetLastError();

@@ -220,7 +220,7 @@ def test_scores_an_fp32_sum_cannot_tell_apart(hga):
     _route_check(sc, sc.batch([0], [64 * 300 - 1]), torch.ones(1, 2, 128, device="cuda"))
 
 
-@pytest.mark.parametrize("pages,copies", [(60, 1), (60, 400), (130, 400), (700, 1), (700, 60)])
+@pytest.mark.parametrize("pages,copies", [(60, 1), (60, 400), (130, 400), (700, 1), (700, 60), (1100, 1)])
 def test_absent_pages_and_odd_summaries(hga, pages, copies):
     """In every form: few tokens and many, short histories and long."""
     sc = Scene(hga, "bf16", 128, 2, 3, lens=(64 * pages, 64 * 20), topk=6, last=2)
