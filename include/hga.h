@@ -704,10 +704,12 @@ int64_t hga_attend_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int3
 
 /* Exact softmax attention of every token over the rows, as stored, of the
  * chunks in its list (or of all its sequence's chunks) at positions up to its
- * own: scores q.k/sqrt(head_dim), natural-log lse as hga_attend's.  A list
- * entry that is negative, beyond the token's own chunk or on an absent page
- * counts for nothing; one that stands twice counts twice.  A token that sees
- * no row (an idle one among them) gets zeros and an lse of -infinity.
+ * own: scores q.k/sqrt(head_dim), natural-log lse as hga_attend's.  Scores,
+ * maxima and sums are held in fp32; a weight enters its product with the values
+ * to 16 bits for bf16 (its rounding 2^-8 of the result's own) and 24 for fp32.
+ * A list entry that is negative, beyond the token's own chunk or on an absent
+ * page counts for nothing; one that stands twice counts twice.  A token that
+ * sees no row (an idle one among them) gets zeros and an lse of -infinity.
  *   q, out      [n_tokens][n_q_heads][head_dim] plan dtype (q strided)
  *   chunk_list  int32 [n_tokens][n_kv_heads][n_list], or NULL with n_list 0
  *   lse         fp32 [n_tokens][n_q_heads] or NULL

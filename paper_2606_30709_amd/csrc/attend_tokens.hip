@@ -10,8 +10,11 @@
 // its tile, and takes those as its reduction indices of the second product: P never leaves the lane.  One pass over the
 // keys with a running reference (the maximum, or up to 2^kSlack below it) and sum of each column, in log2 units.
 //
-// fp32 queries and weights enter the matrix instructions as three bf16 terms each (24 bits); the stored keys and values are
-// exact in bf16.  With up to four query heads the terms are columns of their own (kSpread): column 4 r + x holds term x of
+// The stored keys and values are exact in bf16, and so is a bf16 query.  A bf16 call's weights enter the second product as
+// two bf16 terms each (at most 2^-16 of a weight is left out, against 2^-8 of the result that its own rounding takes; one
+// term would leave out 2^-8 of each weight, which for values of either sign is as much as that rounding: 32 histories up to
+// 32K 57 and 61 us with one term and two, 512 tokens of a 16K prompt 156 and 195).  fp32 queries and weights enter as three
+// terms each (24 bits).  With up to four query heads the terms are columns of their own (kSpread): column 4 r + x holds term x of
 // head r, the scores of four columns are added up, and each multiplies its own term of the weight.  A third of the matrix
 // instructions and half the work of splitting: 1,325 tokens of 12 heads of d64 over 11 pages each 125 -> 105 us.
 //
@@ -40,21 +43,19 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
-__device__ __forceinline__ float low_f32(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high_f32(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // kTerms words whose bf16 pairs add up to (a, b): the rounded values, then what rounding left.
 template <int kTerms>
-__device__ __forceinline__ void split2(float a, float b, uint32_t* w) {
+__device__ __forceinline__ void split2(float a, float b, uint32_t (&w)[kTerms]) {
 #pragma unroll
     for (int i = 0; i < kTerms; ++i) {
         w[i] = pack2(a, b);
-        a -= low_f32(w[i]);
-        b -= high_f32(w[i]);
+        if (i + 1 == kTerms) break;
+        a -= __uint_as_float(w[i] << 16);
+        b -= __uint_as_float(w[i] & 0xffff0000u);
     }
 }
 
-// A lane's share of a page's keys and of its values.
 // The term of a value that column m holds in the spread form: bits 0-7, 8-15 and 16-23 of the significand, counted from the
 // top, each exact in bf16; the fourth column of a head holds zeros.
 struct TermMask {
@@ -76,6 +77,7 @@ __device__ __forceinline__ float quad_sum(float x) {
                    __builtin_amdgcn_mov_dpp(static_cast<int>(__float_as_uint(x)), 0x4E, 0xf, 0xf, true)));
 }
 
+// A lane's share of a page's keys and of its values.
 template <int D>
 struct Keys {
     uint32_t c[4][D / 32];
@@ -205,10 +207,9 @@ __device__ __forceinline__ void page_scores(const Keys<D>& k, const u32x4 (&qf)[
     }
 }
 
-// Its weights under the running reference, four keys of a tile as two words.
-template <int D, int kTerms, int kTiles>
-__device__ __forceinline__ void page_weights(const f32x4 (&sc)[kTiles][4], float scale, Acc<D, kTiles>& acc,
-                                             uint32_t (&w)[kTiles][4][2][kTerms], const TermMask* mask = nullptr) {
+// The running reference of every column, raised where a page's scores exceed it by more than the slack.
+template <int D, int kTiles>
+__device__ __forceinline__ void page_reference(const f32x4 (&sc)[kTiles][4], float scale, Acc<D, kTiles>& acc) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
         float top = sc[i][0][0];
@@ -225,80 +226,89 @@ __device__ __forceinline__ void page_weights(const f32x4 (&sc)[kTiles][4], float
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) acc.o[i][j] *= alpha;
         }
+    }
+}
+
+// The weights of half a page (32 keys, tiles 2 u and 2 u + 1) under the reference, four keys of a tile as two words.
+template <int D, int kParts, int kTiles>
+__device__ __forceinline__ void half_weights(int u, const f32x4 (&sc)[kTiles][4], float scale, Acc<D, kTiles>& acc,
+                                             u32x4 (&w)[kTiles][kParts], const TermMask* mask) {
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
         const float base = acc.m[i] == -INFINITY ? 0.f : acc.m[i];
 #pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
+        for (int b = 0; b < 2; ++b) {
             float pv[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                pv[x] = __builtin_amdgcn_exp2f(fmaf(sc[i][tt][x], scale, -base));
+                pv[x] = __builtin_amdgcn_exp2f(fmaf(sc[i][2 * u + b][x], scale, -base));
                 acc.l[i] += pv[x];
             }
             if (mask) {
 #pragma unroll
                 for (int x = 0; x < 4; ++x) pv[x] = term_of(pv[x], *mask);
                 // exact in bf16: the high halves
-                w[i][tt][0][0] = __builtin_amdgcn_perm(__float_as_uint(pv[1]), __float_as_uint(pv[0]), 0x07060302u);
-                w[i][tt][1][0] = __builtin_amdgcn_perm(__float_as_uint(pv[3]), __float_as_uint(pv[2]), 0x07060302u);
+                w[i][0][2 * b] = __builtin_amdgcn_perm(__float_as_uint(pv[1]), __float_as_uint(pv[0]), 0x07060302u);
+                w[i][0][2 * b + 1] = __builtin_amdgcn_perm(__float_as_uint(pv[3]), __float_as_uint(pv[2]), 0x07060302u);
             } else {
-                split2<kTerms>(pv[0], pv[1], w[i][tt][0]);
-                split2<kTerms>(pv[2], pv[3], w[i][tt][1]);
+                uint32_t lo[kParts], hi[kParts];
+                split2<kParts>(pv[0], pv[1], lo);
+                split2<kParts>(pv[2], pv[3], hi);
+#pragma unroll
+                for (int x = 0; x < kParts; ++x) {
+                    w[i][x][2 * b] = lo[x];
+                    w[i][x][2 * b + 1] = hi[x];
+                }
             }
         }
     }
 }
 
-// Its weighted values: two half pages of 32 keys (tiles 2u, 2u + 1), the rows of a quad decoded two dimensions at a time,
-// then paired by row.
-template <int D, int kTerms, int kTiles>
-__device__ __forceinline__ void page_values(const Values<D>& v, const uint32_t (&w)[kTiles][4][2][kTerms],
+// Its weighted values: the rows of a quad decoded two dimensions at a time, then paired by row.
+template <int D, int kParts, int kTiles>
+__device__ __forceinline__ void half_values(int u, const Values<D>& v, const u32x4 (&w)[kTiles][kParts],
                                             Acc<D, kTiles>& acc) {
     constexpr int DL = D / 16;
+    uint32_t vf[DL][4];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        uint32_t vf[DL][4];
+    for (int b = 0; b < 2; ++b) {
+        const int tt = 2 * u + b;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int tt = 2 * u + b;
+        for (int r2 = 0; r2 < 2; ++r2) {
+            uint32_t lo[DL / 2], hi[DL / 2];
+            const float s0 = scale_of(v.s[tt] >> (16 * r2) & 255u);
+            const float s1 = scale_of(v.s[tt] >> (16 * r2 + 8) & 255u);
+            if constexpr (DL == 8) {
+                const uint32_t c0 = v.c[tt][2 * r2], c1 = v.c[tt][2 * r2 + 1];
+                lo[0] = decode2<0>(c0, s0);
+                lo[1] = decode2<1>(c0, s0);
+                lo[2] = decode2<2>(c0, s0);
+                lo[3] = decode2<3>(c0, s0);
+                hi[0] = decode2<0>(c1, s1);
+                hi[1] = decode2<1>(c1, s1);
+                hi[2] = decode2<2>(c1, s1);
+                hi[3] = decode2<3>(c1, s1);
+            } else {
+                const uint32_t c = v.c[tt][r2];
+                lo[0] = decode2<0>(c, s0);
+                lo[1] = decode2<1>(c, s0);
+                hi[0] = decode2<2>(c, s1);
+                hi[1] = decode2<3>(c, s1);
+            }
 #pragma unroll
-            for (int r2 = 0; r2 < 2; ++r2) {
-                uint32_t lo[DL / 2], hi[DL / 2];
-                const float s0 = scale_of(v.s[tt] >> (16 * r2) & 255u);
-                const float s1 = scale_of(v.s[tt] >> (16 * r2 + 8) & 255u);
-                if constexpr (DL == 8) {
-                    const uint32_t c0 = v.c[tt][2 * r2], c1 = v.c[tt][2 * r2 + 1];
-                    lo[0] = decode2<0>(c0, s0);
-                    lo[1] = decode2<1>(c0, s0);
-                    lo[2] = decode2<2>(c0, s0);
-                    lo[3] = decode2<3>(c0, s0);
-                    hi[0] = decode2<0>(c1, s1);
-                    hi[1] = decode2<1>(c1, s1);
-                    hi[2] = decode2<2>(c1, s1);
-                    hi[3] = decode2<3>(c1, s1);
-                } else {
-                    const uint32_t c = v.c[tt][r2];
-                    lo[0] = decode2<0>(c, s0);
-                    lo[1] = decode2<1>(c, s0);
-                    hi[0] = decode2<2>(c, s1);
-                    hi[1] = decode2<3>(c, s1);
-                }
-#pragma unroll
-                for (int j = 0; j < DL / 2; ++j) {
-                    vf[2 * j][2 * b + r2] = __builtin_amdgcn_perm(hi[j], lo[j], 0x05040100u);
-                    vf[2 * j + 1][2 * b + r2] = __builtin_amdgcn_perm(hi[j], lo[j], 0x07060302u);
-                }
+            for (int j = 0; j < DL / 2; ++j) {
+                vf[2 * j][2 * b + r2] = __builtin_amdgcn_perm(hi[j], lo[j], 0x05040100u);
+                vf[2 * j + 1][2 * b + r2] = __builtin_amdgcn_perm(hi[j], lo[j], 0x07060302u);
             }
         }
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-            for (int x = 0; x < kTerms; ++x) {
-                const u32x4 pf = {w[i][2 * u][0][x], w[i][2 * u][1][x], w[i][2 * u + 1][0][x], w[i][2 * u + 1][1][x]};
-#pragma unroll
-                for (int j = 0; j < DL; ++j)
-                    acc.o[i][j] = mfma(u32x4{vf[j][0], vf[j][1], vf[j][2], vf[j][3]}, pf, acc.o[i][j]);
-            }
     }
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int x = 0; x < kParts; ++x)
+#pragma unroll
+            for (int j = 0; j < DL; ++j)
+                acc.o[i][j] = mfma(u32x4{vf[j][0], vf[j][1], vf[j][2], vf[j][3]}, w[i][x], acc.o[i][j]);
 }
 
 // The weight of a partial result with reference m under the reference `base`.  One without a reference has seen nothing
@@ -319,13 +329,14 @@ constexpr int kResident = kTiles == 2 || kShared || (sizeof(T) == 4 && D == 128 
 // kShared: units of several tokens, from a.units, of which a workgroup may take more than one; else every token is a unit.
 // kSpread: fp32, at most four heads and one token a unit, terms as columns.
 template <typename T, int D, int kTiles, int kWaves, bool kShared, bool kSpread>
-__global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared, kSpread>)) void attend_tokens_kernel(PoolView pool, TokensView tok, AttendArgs a,
-                                                                    const T* __restrict__ q, int64_t q_stride,
-                                                                    T* __restrict__ out, int grid_units) {
+__global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared, kSpread>)) void attend_tokens_kernel(
+    PoolView pool, TokensView tok, AttendArgs a, const T* __restrict__ q, int64_t q_stride, T* __restrict__ out,
+    int grid_units) {
     using F = PageFormat<D>;
     constexpr int kThreads = 64 * kWaves;
     static_assert(!kSpread || (sizeof(T) == 4 && !kShared && kTiles == 1), "");
-    constexpr int kTerms = sizeof(T) == 4 && !kSpread ? 3 : 1;
+    constexpr int kTerms = sizeof(T) == 4 && !kSpread ? 3 : 1;  // of a query
+    constexpr int kParts = sizeof(T) == 2 ? 2 : kTerms;         // of a weight
     constexpr int DL = F::kLaneDims;
     constexpr int kSteps = D / 32;
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(D));  // log2(e) / sqrt(d)
@@ -423,7 +434,8 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared, kSpr
         const auto part = [&](int i, bool any) {
             return make_rsrc(pool.page(__builtin_amdgcn_readlane(mine.id, i)) + h * F::kBytes, any ? F::kBytes : 0);
         };
-        // keys of the next page are fetched once this one's scores are formed, its values once this one's are used
+        // keys of the next page are fetched once this one's scores are formed (with two tiles once half of this one's values
+        // are used too, in their registers), its values once this one's are used
         Keys<D> k;
         Values<D> v;
         {
@@ -443,7 +455,7 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared, kSpr
                 for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
                     for (int x = 0; x < 4; ++x) sc[0][tt][x] = quad_sum(sc[0][tt][x]);
-            load_keys<D>(r, m, g, k);
+            if constexpr (kTiles == 1) load_keys<D>(r, m, g, k);
             if (kShared ? first < c * kPageRows + kPageRows - 1 : __builtin_amdgcn_readlane(mine.rows, cur) < kPageRows) {
                 // rows past a column's position are not seen; those behind the last stored one hold anything, whose
                 // values count as some number (times a weight of 0)
@@ -460,9 +472,18 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared, kSpr
                             if (kShared ? row > pos[i] - c * kPageRows : row >= rows) sc[i][tt][x] = -INFINITY;
                     }
             }
-            uint32_t w[kTiles][4][2][kTerms];
-            page_weights<D, kTerms, kTiles>(sc, scale, acc, w, kSpread ? &terms : nullptr);
-            page_values<D, kTerms, kTiles>(v, w, acc);
+            page_reference<D, kTiles>(sc, scale, acc);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                u32x4 w[kTiles][kParts];
+                half_weights<D, kParts, kTiles>(u, sc, scale, acc, w, kSpread ? &terms : nullptr);
+                if constexpr (kTiles > 1) __builtin_amdgcn_sched_barrier(0);  // or the registers do not suffice
+                half_values<D, kParts, kTiles>(u, v, w, acc);
+                if constexpr (kTiles > 1) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (u == 0) load_keys<D>(r, m, g, k);
+                }
+            }
             load_values<D>(r, m, g, v);
             cur = next;
         }

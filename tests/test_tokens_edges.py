@@ -1,0 +1,60 @@
+"""Single tokens over the paged 4-bit cache where it can go wrong: the precision
+of the weights, rows that are not numbers, keys that pile up at the border of a
+selection, captured steps beside larger ones, wide tables."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import tokens_util as U
+from tokens_util import PAGE, Scene, f64
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def hga():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2606_30709_amd import hga as H
+    H.library()
+    return H
+
+
+# -------------------------------------------------------------- the weights ---
+
+def _rounded_once(sc, q, got, lists=None):
+    """A bf16 result carries one rounding of its own (2^-8 of it at most).  What
+    comes before is in proportion to sum p |v| / l: a score's error as in
+    tokens_util.attend_tolerance, the sums', and the weight's.  That one enters
+    the product as two bf16 terms: the first leaves at most 2^-8 of it, the second
+    2^-8 of that."""
+    k, v = sc.k_v()
+    ln = None if lists is None else lists.cpu().numpy()
+    ref, _, mag, reach, count = U.attend(f64(q), k, v, sc.table, sc.seq, sc.pos, sc.kv, ln, sc.n_ids)
+    u = 2.0 ** -24
+    rel = 2 * (2 * (sc.d + 12) * u * reach + 8 * u) + 2 * count * u + 2.0 ** -16
+    before = rel[..., None] * mag
+    err = np.abs(f64(got[0]) - ref)
+    tol = before + 2.0 ** -8 * (np.abs(ref) + before) + 1e-30
+    assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("d,kv,ratio", [(128, 4, 8), (64, 3, 3), (64, 1, 16), (128, 5, 2), (128, 1, 1)])
+def test_bf16_results_are_rounded_once(hga, d, kv, ratio):
+    """Weights of about the same size over values of either sign: results far
+    below the values, which a weight of eight bits would not carry.  In the
+    forms of one token a unit, of several (one tile and two), of lists."""
+    lens = (64, 130, 300, 7, 1)
+    sc = Scene(hga, "bf16", d, kv, ratio, lens=lens, seed=11)
+    single = sc.batch(range(5), [n - 1 for n in lens])
+    q = sc.random(5, sc.hq, d, scale=0.05)
+    _rounded_once(sc, q, sc.attend(single, q))
+    lists = torch.from_numpy(np.tile(np.int32([0, 1, -1, 4]), (5, kv, 1))).cuda()
+    _rounded_once(sc, q, sc.attend(single, q, lists), lists)
+    for n in (3, 60):
+        seq, pos = [0] * n + [1] * n + [2] * n, [*range(64 - n, 64), *range(130 - n, 130), *range(200, 200 + n)]
+        q = sc.random(3 * n, sc.hq, d, scale=0.05)
+        _rounded_once(sc, q, sc.attend(sc.batch(seq, pos), q))
