@@ -217,7 +217,10 @@ __device__ __forceinline__ Border find_border(const uint64_t* keys, int n, int k
     }
     __syncthreads();
     const int bin = s.bin, need = k - s.above, in = static_cast<int>(s.hist[bin]);
-    if (in > kThreads) return border_by_bytes(keys, n, k, s);
+    if (in > kThreads) {
+        __syncthreads();  // every thread has read its count before the counts are cleared for bytes
+        return border_by_bytes(keys, n, k, s);
+    }
     for (int i = tid; i < n; i += kThreads) {
         const uint64_t v = keys[i];
         if (v != 0 && bin_of(v) == bin) {

@@ -9,7 +9,8 @@ import pytest
 import torch
 
 import tokens_util as U
-from tokens_util import PAGE, Scene, f64
+from test_tokens import _route_check
+from tokens_util import Scene, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +59,25 @@ def test_bf16_results_are_rounded_once(hga, d, kv, ratio):
         seq, pos = [0] * n + [1] * n + [2] * n, [*range(64 - n, 64), *range(130 - n, 130), *range(200, 200 + n)]
         q = sc.random(3 * n, sc.hq, d, scale=0.05)
         _rounded_once(sc, q, sc.attend(sc.batch(seq, pos), q))
+
+
+# -------------------------------------------------------------- the routing ---
+
+@pytest.mark.parametrize("tokens", [1, 70])
+@pytest.mark.parametrize("low", ["close", "equal", "two"])
+def test_more_keys_at_the_border_than_a_workgroup_ranks(hga, tokens, low):
+    """More than 512 low scores under a few high ones, the border among them:
+    apart from one another, equal, or of two values.  With one token the scores
+    are formed by the whole device, with more by a workgroup a token and head."""
+    pages = 1100
+    sc = Scene(hga, "f32", 64, 2, 1, lens=(64 * pages,), topk=20, seed=12)
+    x = {"close": 1.0 + sc.rng.permutation(pages) * 1e-6, "equal": np.ones(pages),
+         "two": 1.0 + (np.arange(pages) % 2) * 1e-3}[low]
+    x[[30, 500, 1000]] = [1000.0, 900.0, 1000.0]
+    sums = np.zeros((pages, 2, 64), np.float32)
+    sums[:, 0, 3], sums[:, 1, 60] = x, -x[::-1]
+    sc.pool.page_sum[0, torch.from_numpy(sc.table[0]).long()] = torch.from_numpy(sums).cuda()
+    q = torch.zeros(tokens, 2, 64, device="cuda")
+    q[:, 0, 3], q[:, 1, 60] = 1.0, -1.0
+    pos = [64 * pages - 1 - i for i in range(tokens)]
+    _route_check(sc, sc.batch([0] * tokens, pos), q)
