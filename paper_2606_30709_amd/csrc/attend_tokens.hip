@@ -311,6 +311,40 @@ __device__ __forceinline__ void half_values(int u, const Values<D>& v, const u32
                 acc.o[i][j] = mfma(u32x4{vf[j][0], vf[j][1], vf[j][2], vf[j][3]}, w[i][x], acc.o[i][j]);
 }
 
+// Value blocks of a page that stand for NaN, where some columns see a row and others do not: 0 * NaN would reach those too.
+// They count as some number from here on, and the columns that see them become NaN (the block's dimensions): column
+// 16 i + m sees the page's rows up to seen[i].
+template <int D, int kTiles>
+__device__ __forceinline__ void take_out_nan(Values<D>& v, int m, int g, const int (&seen)[kTiles], Acc<D, kTiles>& acc) {
+    constexpr int DL = D / 16;
+    const auto bytes_255 = [](uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u; };
+    uint32_t any = 0;
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt) any |= bytes_255(v.s[tt]);
+    if (!__builtin_amdgcn_ballot_w64(any != 0)) return;
+    uint32_t reached = 0;  // bit i: column 16 i + m, in the lane's dimensions (a block's: (4 g + x) DL + j, x < 4, j < DL)
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt) {
+        const uint32_t is = bytes_255(v.s[tt]);
+        for (int x = 0; x < 4; ++x) {
+            // one lane for a block's: those of its first dimensions
+            uint64_t lanes = __builtin_amdgcn_ballot_w64((is >> (8 * x) & 0x80u) != 0 && m * DL % 32 == 0);
+            for (; lanes; lanes &= lanes - 1) {
+                const int at = static_cast<int>(__builtin_ctzll(lanes)), row = 16 * tt + 4 * (at >> 4) + x;
+                if ((at & 15) * DL / 32 != 4 * g * DL / 32) continue;
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i) reached |= row <= seen[i] ? 1u << i : 0u;
+            }
+        }
+        v.s[tt] ^= is;  // 127, a scale of 1
+    }
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+        if (reached >> i & 1)
+#pragma unroll
+            for (int j = 0; j < DL; ++j) acc.o[i][j] = f32x4{NAN, NAN, NAN, NAN};
+}
+
 // The weight of a partial result with reference m under the reference `base`.  One without a reference has seen nothing
 // (zeros) or only what is not a number: that stays.
 __device__ __forceinline__ float part_weight(float m, float base) {
@@ -471,6 +505,12 @@ __global__ __launch_bounds__(64 * kWaves, (kResident<T, D, kTiles, kShared, kSpr
                         for (int i = 0; i < kTiles; ++i)
                             if (kShared ? row > pos[i] - c * kPageRows : row >= rows) sc[i][tt][x] = -INFINITY;
                     }
+                if constexpr (kShared) {
+                    int seen[kTiles];
+#pragma unroll
+                    for (int i = 0; i < kTiles; ++i) seen[i] = pos[i] - c * kPageRows;
+                    take_out_nan<D, kTiles>(v, m, g, seen, acc);
+                }
             }
             page_reference<D, kTiles>(sc, scale, acc);
 #pragma unroll

@@ -61,6 +61,42 @@ def test_bf16_results_are_rounded_once(hga, d, kv, ratio):
         _rounded_once(sc, q, sc.attend(sc.batch(seq, pos), q))
 
 
+# --------------------------------------------------- rows that are not numbers ---
+
+@pytest.mark.parametrize("dtype,d,kv,ratio,n", [
+    ("bf16", 128, 2, 8, 3), ("bf16", 128, 2, 8, 70), ("bf16", 64, 1, 1, 100), ("bf16", 64, 2, 16, 5),
+    ("bf16", 64, 1, 3, 200), ("f32", 128, 2, 2, 40), ("f32", 64, 2, 4, 70), ("f32", 64, 1, 16, 4)])
+@pytest.mark.parametrize("pages", [3, 60])
+def test_a_value_that_is_no_number_reaches_later_tokens_only(hga, dtype, d, kv, ratio, n, pages):
+    """Value blocks that stand for NaN among the rows of a call's own tokens
+    (tokens that share their pages, from one page to several behind, few pages and
+    many): in the block's dimensions, tokens from that row on are NaN, and nothing
+    else is, with a workspace (of any size) as without."""
+    sc = Scene(hga, dtype, d, kv, ratio, lens=(64 * pages + 20, 40), seed=13)
+    last = sc.lens[0]
+    _, _, _, vs = U.addresses(d)
+    clean = sc.k_v()
+    # (position, head, block): the first and last of the call's tokens, one before them all, one twice in a row
+    bad = [(last - n // 2, 0, 0), (last - 1, kv - 1, d // 32 - 1), (last - n + 1, 0, d // 32 - 1),
+           (last - n // 3, kv - 1, 1), (last - n // 3, kv - 1, 0)]
+    for p, h, b in bad:
+        sc.pool.pages[0, int(sc.table[0, p // 64]), h, int(vs[p % 64, 32 * b])] = 255
+    seq, pos = np.array([0] * n + [1] * 3), np.array([*range(last - n, last), 3, 39, 20])
+    batch = sc.batch(seq, pos)
+    q = sc.random(n + 3, sc.hq, d)
+    want = np.zeros((n + 3, sc.hq, d), bool)
+    for p, h, b in bad:
+        want[:n][pos[:n] >= p, h * ratio:(h + 1) * ratio, 32 * b:32 * b + 32] = True
+    ref, rlse, mag, reach, count = U.attend(f64(q), *clean, sc.table, seq, pos, kv, None, sc.n_ids)
+    tol, ltol = U.attend_tolerance(dtype, d, ref, mag, reach, count)
+    for ws in (True, 4 * (n + 3) + 32, False):
+        out, lse = sc.attend(batch, q, workspace=ws)
+        o, l = f64(out), f64(lse)
+        assert np.array_equal(np.isnan(o), want)
+        assert ((np.abs(o - ref) <= tol) | want).all()
+        assert (np.abs(l - rlse) <= ltol).all()
+
+
 # -------------------------------------------------------------- the routing ---
 
 @pytest.mark.parametrize("tokens", [1, 70])
