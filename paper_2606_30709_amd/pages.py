@@ -215,7 +215,9 @@ class PagedCache:
             self.page_table.view(-1).index_copy_(0, up[0], up[1].int())
 
     def append(self, seqs, counts) -> hga.TokenBatch:
-        """The next counts[i] tokens of sequence seqs[i], in order."""
+        """The next counts[i] tokens of sequence seqs[i], in order.  The batch's
+        tensors are new ones: for a captured step copy its tok_seq and tok_pos
+        into those of the batch it was captured with."""
         seqs, counts = np.asarray(seqs, np.int64).reshape(-1), np.asarray(counts, np.int64).reshape(-1)
         moves = self.book.append(seqs, counts)
         self._apply(moves)

@@ -530,18 +530,32 @@ class TokenPipeline:
     """One layer's attention of a batch of tokens over a ``PagedCache``: their
     rows appended, each token routed to its own chunks (or, with ``routed``
     false, given all of them) and attended.  Buffers are those of the largest
-    batch so far, so that a step of a size seen before allocates nothing (and
-    may be captured into a graph)."""
+    batch so far, so that a step of a size seen before allocates nothing and
+    may be captured into a graph; one that would have to allocate is refused
+    while a stream captures.  What a captured step uses is kept for the
+    pipeline's life, whatever larger steps come later: replays need the pipeline
+    (and the batch's tensors) alive, and the steps and replays of one pipeline
+    in an order, since they share its buffers."""
 
     def __init__(self, cache, routed: bool = True):
         self.cache, self.plan, self.routed = cache, cache.plan, routed
         self._buf = {}
+        self._captured = {}  # by address: buffers that a graph may hold
 
     def _buffer(self, name, shape, dtype):
         n = int(np.prod(shape))
         t = self._buf.get(name)
+        capturing = torch.cuda.is_current_stream_capturing()
         if t is None or t.numel() < n:
+            if capturing:
+                raise hga.HgaError(-1, "HGA_EINVAL: a captured step has to be of a size that ran "
+                                       f"before ('{name}' would be allocated)")
+            if t is not None and t.is_cuda:
+                # its last use may be on another stream than the one it was allocated on
+                t.record_stream(torch.cuda.current_stream(t.device))
             t = self._buf[name] = torch.empty(max(n, 1), dtype=dtype, device=self.cache.pool.device)
+        if capturing:
+            self._captured[t.data_ptr()] = t
         return t[:n].view(shape)
 
     def step(self, layer: int, batch: hga.TokenBatch, q, k, v):
@@ -550,19 +564,20 @@ class TokenPipeline:
         step.  Runs on the current stream."""
         p, plan, pool = self.plan.params, self.plan, self.cache.pool
         T = batch.n_tokens
+        # every buffer before the first launch
         out = self._buffer("out", (T, p.n_q_heads, p.head_dim), plan.torch_dtype)
         lse = self._buffer("lse", (T, p.n_q_heads), torch.float32)
-        hga.hga_cache_append(plan, pool, layer, batch, k, v)
-        lists = None
+        lists = route = attend = None
         if self.routed:
             lists = self._buffer("lists", (T, p.n_kv_heads, hga.hga_token_list_size(plan)),
                                  torch.int32)
             nbytes = hga.hga_route_tokens_workspace(plan, batch)
-            hga.hga_route_tokens(plan, pool, layer, batch, q, lists,
-                                 workspace=self._buffer("route", (nbytes,), torch.uint8)
-                                 if nbytes else None)
+            route = self._buffer("route", (nbytes,), torch.uint8) if nbytes else None
         nbytes = hga.hga_attend_tokens_workspace(plan, batch, lists)
+        attend = self._buffer("attend", (nbytes,), torch.uint8) if nbytes else None
+        hga.hga_cache_append(plan, pool, layer, batch, k, v)
+        if self.routed:
+            hga.hga_route_tokens(plan, pool, layer, batch, q, lists, workspace=route)
         hga.hga_attend_tokens(plan, pool, layer, batch, q, out, lse=lse, chunk_list=lists,
-                              workspace=self._buffer("attend", (nbytes,), torch.uint8)
-                              if nbytes else None)
+                              workspace=attend)
         return out, lse

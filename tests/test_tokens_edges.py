@@ -117,3 +117,54 @@ def test_more_keys_at_the_border_than_a_workgroup_ranks(hga, tokens, low):
     q[:, 0, 3], q[:, 1, 60] = 1.0, -1.0
     pos = [64 * pages - 1 - i for i in range(tokens)]
     _route_check(sc, sc.batch([0] * tokens, pos), q)
+
+
+# ------------------------------------------------------------ captured steps ---
+
+@pytest.mark.parametrize("routed", [True, False])
+def test_a_captured_step_beside_larger_ones(hga, routed):
+    """A decode step captured, a prompt run through the same pipeline, memory
+    allocated and filled where its buffers might have been; then replays for the
+    next tokens, against a pipeline of their own, and the filled memory as it
+    was."""
+    from paper_2606_30709_amd.pages import PagedCache
+    from paper_2606_30709_amd.pipeline import TokenPipeline
+    plan = hga.Plan(batch=1, n_q_heads=8, n_kv_heads=2, head_dim=128, keep_first=1, keep_last=1, topk_chunks=3,
+                    topk_groups=4)
+    cache = PagedCache(plan, 300, 4, 80, n_layers=2)
+    pipe, other = TokenPipeline(cache, routed), TokenPipeline(cache, routed)
+    g = torch.Generator().manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=g).bfloat16().cuda()  # noqa: E731
+
+    def prompt(seqs, counts):
+        b = cache.append(seqs, counts)
+        for layer in (0, 1):
+            pipe.step(layer, b, rand(b.n_tokens, 8, 128), rand(b.n_tokens, 2, 128), rand(b.n_tokens, 2, 128))
+
+    prompt([0, 1, 2], [40, 4500, 30])
+    pipe = TokenPipeline(cache, routed)  # of small steps so far
+    batch = cache.append([0, 1, 2], [1, 1, 1])
+    q, k, v = rand(3, 8, 128), rand(3, 2, 128), rand(3, 2, 128)
+    step = lambda p: [p.step(layer, batch, q, k, v) for layer in (0, 1)][1]  # noqa: E731
+    step(pipe)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = step(pipe)
+    addresses = {t.data_ptr() for t in pipe._buf.values()}
+    prompt([3], [700])
+    assert not addresses & {t.data_ptr() for t in pipe._buf.values()}
+    filled = [torch.full((n,), 77, dtype=torch.uint8, device="cuda") for n in [512] * 200 + [2 ** 20] * 40 + [2 ** 22] * 8]
+    for _ in range(4):
+        b = cache.append([0, 1, 2], [1, 1, 1])
+        batch.tok_seq.copy_(b.tok_seq)
+        batch.tok_pos.copy_(b.tok_pos)
+        for x in (q, k, v):
+            x.copy_(rand(*x.shape))
+        graph.replay()
+        want = step(other)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        assert all(bool((t == 77).all()) for t in filled)
+    with pytest.raises(hga.HgaError):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            step(TokenPipeline(cache, routed))
