@@ -674,9 +674,9 @@ hga_status hga_cache_append(const hga_plan* plan, const hga_pool* pool, int32_t 
 hga_status hga_cache_read(const hga_plan* plan, const hga_pool* pool, int32_t layer,
                           const hga_tokens* tokens, void* k_out, void* v_out, void* stream);
 
-/* Bytes hga_route_tokens makes use of (up to 16384 pages it does without them,
- * but takes longer over long histories of few tokens), or a negative
- * hga_status.  Host only. */
+/* Bytes hga_route_tokens makes use of: at most 2^28, or one token's (up to 16384
+ * pages it does without them, but takes longer over long histories of few
+ * tokens), or a negative hga_status.  Host only. */
 int64_t hga_route_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int32_t max_pages);
 
 /* Route every token by itself (Sec. 3.3 at the grain of a token): with c the
@@ -689,9 +689,11 @@ int64_t hga_route_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int32
  *   q           [n_tokens][n_q_heads][head_dim] plan dtype (strided)
  *   chunk_list  int32 [n_tokens][n_kv_heads][n_list], ascending, padded with
  *               -1 (all of an idle token's); n_list >= hga_token_list_size
- *   workspace   hga_route_tokens_workspace bytes, or (up to 16384 pages) NULL
- *               and 0; calls that overlap in time (graphs replayed side by side
- *               among them) need one each.  The lists do not depend on it. */
+ *   workspace   hga_route_tokens_workspace bytes (above 16384 pages a call of
+ *               many tokens goes through them in parts, fewer if there are
+ *               more bytes), or, up to 16384 pages, NULL and 0; calls that
+ *               overlap in time (graphs replayed side by side among them) need
+ *               one each.  The lists do not depend on it. */
 hga_status hga_route_tokens(const hga_plan* plan, const hga_pool* pool, int32_t layer,
                             const hga_tokens* tokens, const void* q, int64_t q_stride,
                             int32_t* chunk_list, int32_t n_list, void* workspace,

@@ -11,7 +11,7 @@
 //   a wavefront a unit    many units of short histories (prompts): keys in registers, no barrier
 //   a workgroup a unit    keys in LDS
 //   two kernels           few units of long histories: their scores by workgroups of kSlice rows each, keys in the
-//                         workspace; then the choice, a workgroup a unit
+//                         workspace; then the choice, a workgroup a unit; as many tokens at a time as the workspace holds
 #include <algorithm>
 
 #include "hga_device.hpp"
@@ -28,6 +28,9 @@ constexpr int kLdsPages = 1 << 14;
 // Pages of a sequence up to which a wavefront takes a unit: keys a lane.
 constexpr int kLaneKeys = 4;
 constexpr int kSlice = 128;  // rows of a scoring workgroup of the two-kernel form
+// Bytes of keys that the two-kernel form asks for, or one token's: a call of more tokens takes them in parts.  (A page
+// table may be wide for the sake of one sequence: 4,096 tokens of 4 heads at 2^18 pages would have 32 GiB of keys.)
+constexpr int64_t kKeyBytes = int64_t(1) << 28;
 
 // A key that orders as the score: 0 is no candidate, 1 a score that is not a number.
 __device__ __forceinline__ uint64_t score_key(double s) {
@@ -520,16 +523,28 @@ bool few_and_long(const hga_plan& plan, int64_t units, int max_pages) {
 
 template <typename T, int D>
 hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const RouteArgs& a, const void* q,
-               int64_t q_stride, int32_t* list, uint64_t* ws, hipStream_t stream) {
+               int64_t q_stride, int32_t* list, uint64_t* ws, int64_t ws_tokens, hipStream_t stream) {
     const int64_t units = static_cast<int64_t>(tok.n_tokens) * pool.n_kv;
     const T* qt = static_cast<const T*>(q);
     if (ws) {
         const int slices = (tok.max_pages + kSlice - 1) / kSlice;
-        score_slices_kernel<T, D><<<grid_of(units * slices, 256), 256, 0, stream>>>(pool, tok, a, slices, qt, q_stride, ws);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        choose_kernel<<<grid_of(units, kThreads), kThreads, 0, stream>>>(pool, tok, a, ws, list);
-        return hipGetLastError();
+        const int64_t part = std::min(ws_tokens, (int64_t(1) << 30) / (static_cast<int64_t>(slices) * pool.n_kv));
+        for (int64_t t = 0; t < tok.n_tokens; t += part) {
+            TokensView some = tok;
+            some.seq += t;
+            some.pos += t;
+            some.n_tokens = static_cast<int>(std::min(part, tok.n_tokens - t));
+            const int64_t n = static_cast<int64_t>(some.n_tokens) * pool.n_kv;
+            score_slices_kernel<T, D><<<grid_of(n * slices, 256), 256, 0, stream>>>(pool, some, a, slices,
+                                                                                   qt + t * q_stride, q_stride, ws);
+            hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            choose_kernel<<<grid_of(n, kThreads), kThreads, 0, stream>>>(pool, some, a, ws,
+                                                                         list + t * pool.n_kv * a.n_list);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     }
     // A wavefront a unit: up to 64 chunks, a key a lane, at any count (3 heads of d64 at 4K, 1 token: 4.9 us, 6.6 with a
     // workgroup; 330 tokens: 5.7 and 12.5); up to four keys a lane where the units fill the device (1 token at 8K: 7.1 and
@@ -554,10 +569,16 @@ hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok
 
 }  // namespace
 
+// Bytes of a token's keys in the two-kernel form.
+static int64_t token_key_bytes(const hga_plan& plan, int max_pages) {
+    return static_cast<int64_t>(plan.p.n_kv_heads) * max_pages * static_cast<int64_t>(sizeof(uint64_t));
+}
+
 int64_t route_tokens_bytes(const hga_plan& plan, int n_tokens, int max_pages, bool must) {
     const int64_t units = static_cast<int64_t>(n_tokens) * plan.p.n_kv_heads;
     if (must ? max_pages <= kLdsPages : !few_and_long(plan, units, max_pages)) return 0;
-    return units * max_pages * static_cast<int64_t>(sizeof(uint64_t));
+    const int64_t one = token_key_bytes(plan, max_pages);
+    return std::min<int64_t>(n_tokens, std::max<int64_t>(1, kKeyBytes / one)) * one;
 }
 
 hipError_t launch_route_tokens(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const void* q,
@@ -574,7 +595,8 @@ hipError_t launch_route_tokens(const hga_plan& plan, const PoolView& pool, const
     const bool f32 = plan.p.dtype == HGA_F32;
     const auto f = plan.p.head_dim == 128 ? (f32 ? run<float, 128> : run<bf16_t, 128>)
                                           : (f32 ? run<float, 64> : run<bf16_t, 64>);
-    return f(plan, pool, tok, a, q, q_stride, list, keys, stream);
+    return f(plan, pool, tok, a, q, q_stride, list, keys, keys ? ws_bytes / token_key_bytes(plan, tok.max_pages) : 0,
+             stream);
 }
 
 }  // namespace hga

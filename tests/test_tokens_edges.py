@@ -119,6 +119,34 @@ def test_more_keys_at_the_border_than_a_workgroup_ranks(hga, tokens, low):
     _route_check(sc, sc.batch([0] * tokens, pos), q)
 
 
+def test_many_tokens_through_a_wide_table(hga):
+    """A table of 20,000 pages a sequence, for the sake of one: the keys' workspace
+    stays small, and a call whose units it does not hold goes through it in parts."""
+    from types import SimpleNamespace
+    sc = Scene(hga, "bf16", 64, 3, 2, lens=(64 * 30, 64 * 500, 70), topk=6, max_pages=20000, seed=14)
+    for n, pages in ((4096, 1 << 18), (1 << 20, 1 << 18), (700, 20000), (1 << 28, 16385)):
+        assert 0 < hga.hga_route_tokens_workspace(sc.plan, SimpleNamespace(n_tokens=n, max_pages=pages)) <= 1 << 28
+    sc.table[1] = sc.table[1, sc.rng.integers(0, 500, 20000)]  # over pages that recur
+    n = 700                                                     # of which a part holds 559
+    seq = np.array([0] * 690 + [1] * 2 + [2] * 8)
+    pos = np.array([*range(64 * 30 - 690, 64 * 30), 64 * 19000 + 5, 64 * 20000 - 1, *range(62, 70)])
+    order = sc.rng.permutation(n)
+    batch = sc.batch(seq[order], pos[order])
+    q = sc.random(n, sc.hq, 64)
+    nb = hga.hga_route_tokens_workspace(sc.plan, batch)
+    assert nb < 8 * 3 * n * 20000
+    _route_check(sc, batch, q)
+    # ... and in one part, to the same lists; a workspace below what is asked for is refused
+    lists = [torch.full((n, 3, hga.hga_token_list_size(sc.plan)), -7, dtype=torch.int32, device="cuda") for _ in range(2)]
+    for out, nbytes in zip(lists, (nb, 8 * 3 * n * 20000)):
+        hga.hga_route_tokens(sc.plan, sc.pool, 0, batch, q, out,
+                             workspace=torch.empty(nbytes, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(*lists)
+    with pytest.raises(hga.HgaError):
+        hga.hga_route_tokens(sc.plan, sc.pool, 0, batch, q, lists[0],
+                             workspace=torch.empty(nb - 16, dtype=torch.uint8, device="cuda"))
+
+
 # ------------------------------------------------------------ captured steps ---
 
 @pytest.mark.parametrize("routed", [True, False])
