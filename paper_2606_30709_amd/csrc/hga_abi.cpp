@@ -202,9 +202,12 @@ hga_status hga_plan_create(const hga_params* params, hga_plan** plan) {
         return fail(HGA_EUNSUPPORTED, "hf_pairs_chunk (%d) below hf_pairs_group (%d) is not "
                     "supported: a high-frequency group pair must be high-frequency for the chunk",
                     p.hf_pairs_chunk, p.hf_pairs_group);
-    const std::vector<float> tg = phase_table(p.group, p.head_dim, p.rope_base, p.hf_pairs_group);
-    const std::vector<float> tc = psi_table(p.chunk, p.group, p.head_dim, p.rope_base);
-    const std::vector<float> tp = phase_table(p.chunk, p.head_dim, p.rope_base, p.hf_pairs_chunk);
+    // the phase tables one behind the other: a group's, psi, and a page's (hga::phase_chunk)
+    std::vector<float> tables = phase_table(p.group, p.head_dim, p.rope_base, p.hf_pairs_group);
+    const size_t n_group = tables.size();
+    for (const std::vector<float>& t : {psi_table(p.chunk, p.group, p.head_dim, p.rope_base),
+                                        phase_table(p.chunk, p.head_dim, p.rope_base, p.hf_pairs_chunk)})
+        tables.insert(tables.end(), t.begin(), t.end());
 
     int dev = -1;
     hipError_t e = hipGetDevice(&dev);
@@ -226,25 +229,20 @@ hga_status hga_plan_create(const hga_params* params, hga_plan** plan) {
     pl->max_lds = max_lds;
     pl->n_cu = n_cu;
     float* buf = nullptr;
-    // the page's table behind the two that the plan names (hga::phase_chunk)
-    const size_t bytes = (tc.size() + tg.size() + tp.size()) * sizeof(float);
+    const size_t bytes = tables.size() * sizeof(float);
     e = hipMalloc(&buf, bytes);
     if (e != hipSuccess) {
         delete pl;
         return hip_fail(e, "hipMalloc (phase tables)");
     }
-    e = hipMemcpy(buf, tg.data(), tg.size() * sizeof(float), hipMemcpyHostToDevice);
-    if (e == hipSuccess)
-        e = hipMemcpy(buf + tg.size(), tc.data(), tc.size() * sizeof(float), hipMemcpyHostToDevice);
-    if (e == hipSuccess)
-        e = hipMemcpy(buf + tg.size() + tc.size(), tp.data(), tp.size() * sizeof(float), hipMemcpyHostToDevice);
+    e = hipMemcpy(buf, tables.data(), bytes, hipMemcpyHostToDevice);
     if (e != hipSuccess) {
         (void)hipFree(buf);
         delete pl;
         return hip_fail(e, "hipMemcpy (phase tables)");
     }
     pl->phase_group = buf;
-    pl->phase_psi = buf + tg.size();
+    pl->phase_psi = buf + n_group;
     // the spread routing form's workspace: keys, then per-unit counters that
     // start at zero (each call leaves them at zero)
     void* ws = nullptr;
