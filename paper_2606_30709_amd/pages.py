@@ -3,12 +3,12 @@
 ``PageBook`` is the host's part: which page holds which chunk of which
 sequence, how many sequences share a page, which pages are free.  It touches no
 device.  ``PagedCache`` keeps a pool and a page table on the GPU in step with
-it, with ``hga_copy_pages`` for what has to move.
+it, with ``hga_copy_pages`` for what has to move, whichever device is current.
 
 A page is shared by the sequences that were forked from one another until one
 of them appends to it; that one then gets a copy of its own.  All device work
-runs on the current stream, so a page that one call frees may be written by the
-next.
+runs on the device's current stream, so a page that one call frees may be
+written by the next.
 """
 
 from __future__ import annotations
@@ -204,6 +204,11 @@ class PagedCache:
         return t.to(self.pool.device, non_blocking=True)
 
     def _apply(self, moves):
+        # the calls ask for the pool's device to be the current one, and the book has changed already
+        with torch.cuda.device(self.pool.index):
+            self._write(moves)
+
+    def _write(self, moves):
         if moves:
             m = self._upload(np.asarray(moves, np.int32).T)
             hga.hga_copy_pages(self.plan, self.pool, m[0], m[1])
