@@ -44,12 +44,14 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-// kTerms words whose bf16 pairs add up to (a, b): the rounded values, then what rounding left.
+// kTerms words whose bf16 pairs add up to (a, b): the rounded values, then what rounding left.  The first of three terms is
+// cut off instead, which leaves no more than the other two hold: rounded, the largest floats would become infinite.
 template <int kTerms>
 __device__ __forceinline__ void split2(float a, float b, uint32_t (&w)[kTerms]) {
 #pragma unroll
     for (int i = 0; i < kTerms; ++i) {
-        w[i] = pack2(a, b);
+        w[i] = kTerms == 3 && i == 0 ? __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u)
+                                     : pack2(a, b);
         if (i + 1 == kTerms) break;
         a -= __uint_as_float(w[i] << 16);
         b -= __uint_as_float(w[i] & 0xffff0000u);

@@ -61,6 +61,22 @@ def test_bf16_results_are_rounded_once(hga, d, kv, ratio):
         _rounded_once(sc, q, sc.attend(sc.batch(seq, pos), q))
 
 
+@pytest.mark.parametrize("d,ratio", [(64, 1), (64, 5), (128, 4), (128, 16)])
+def test_the_largest_fp32_queries(hga, d, ratio):
+    """Queries up to the largest float over keys as small: scores of ordinary size."""
+    sc = Scene(hga, "f32", d, 2, ratio, lens=(200, 70, 330), seed=15)
+    ks = U.addresses(d)[1]
+    sc.bytes[..., ks] = 2  # 2^-125
+    sc.pool.pages[0].copy_(torch.from_numpy(sc.bytes))
+    for seq, pos in (([0, 1, 2], [199, 69, 329]), ([0] * 9 + [2] * 40, [*range(191, 200), *range(290, 330)])):
+        q = sc.random(len(seq), sc.hq, d)
+        q = q * (2.0 ** 124 / d ** 0.5)
+        q[:, :, 3], q[:, ::2, 17] = torch.finfo(torch.float32).max, -torch.finfo(torch.float32).max
+        batch = sc.batch(seq, pos)
+        sc.check_attend(q, sc.attend(batch, q))
+        sc.check_attend(q, sc.attend(batch, q, workspace=False))
+
+
 # --------------------------------------------------- rows that are not numbers ---
 
 @pytest.mark.parametrize("dtype,d,kv,ratio,n", [
