@@ -621,6 +621,11 @@ int32_t hga_visible_chunks(const hga_params* params, int32_t c, int32_t* chunks,
  * page_table is [n_seqs][max_pages], max_pages <= 2^18.  What is read of these
  * device arrays is checked by the kernels: no id leads outside the pool.
  *
+ * A call takes the form that suits n_tokens, n_seqs and max_pages: the host
+ * does not know the histories' lengths.  The results do not depend on it but
+ * for the order of sums; the time does (a table much wider than its histories,
+ * or with many more rows than the call has sequences, costs some of it).
+ *
  * The plan gives heads, head_dim, dtype, the rotary phases and the routing
  * parameters (keep_first, keep_last, force_prev, topk_chunks); its batch and
  * topk_groups play no part.  Rows of q, k and v may be strided: x_stride
@@ -709,6 +714,8 @@ int64_t hga_attend_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int3
  * own: scores q.k/sqrt(head_dim), natural-log lse as hga_attend's.  Scores,
  * maxima and sums are held in fp32; a weight enters its product with the values
  * to 16 bits for bf16 (its rounding 2^-8 of the result's own) and 24 for fp32.
+ * (Before the division by their sum weights are up to 2^8: values above 2^119
+ * over the number of rows may pass fp32's range.)
  * A list entry that is negative, beyond the token's own chunk or on an absent
  * page counts for nothing; one that stands twice counts twice.  A token that
  * sees no row (an idle one among them) gets zeros and an lse of -infinity.
@@ -718,7 +725,8 @@ int64_t hga_attend_tokens_workspace(const hga_plan* plan, int32_t n_tokens, int3
  *   workspace   any size (hga_attend_tokens_workspace bytes to let long
  *               histories of few tokens spread over the device), or NULL and
  *               0; calls that overlap in time need one each.  Its size decides
- *               the order of the sums, its contents nothing. */
+ *               the order of the sums (and which tokens share a tile), its
+ *               contents nothing. */
 hga_status hga_attend_tokens(const hga_plan* plan, const hga_pool* pool, int32_t layer,
                              const hga_tokens* tokens, const void* q, int64_t q_stride,
                              const int32_t* chunk_list, int32_t n_list, void* out, float* lse,

@@ -11,12 +11,12 @@
 // keys with a running reference (the maximum, or up to 2^kSlack below it) and sum of each column, in log2 units.
 //
 // The stored keys and values are exact in bf16, and so is a bf16 query.  A bf16 call's weights enter the second product as
-// two bf16 terms each (at most 2^-16 of a weight is left out, against 2^-8 of the result that its own rounding takes; one
-// term would leave out 2^-8 of each weight, which for values of either sign is as much as that rounding: 32 histories up to
-// 32K 57 and 61 us with one term and two, 512 tokens of a 16K prompt 156 and 195).  fp32 queries and weights enter as three
-// terms each (24 bits).  With up to four query heads the terms are columns of their own (kSpread): column 4 r + x holds term x of
-// head r, the scores of four columns are added up, and each multiplies its own term of the weight.  A third of the matrix
-// instructions and half the work of splitting: 1,325 tokens of 12 heads of d64 over 11 pages each 125 -> 105 us.
+// two bf16 terms each: at most 2^-16 of a weight is left out, against 2^-8 of the result that its own rounding takes.  One
+// term would leave out 2^-8 of each weight, which for values of either sign is as much as that rounding (32 histories up to
+// 32K 57 and 61 us with one term and two, 512 tokens of a 16K prompt 156 and 198).  fp32 queries and weights enter as three
+// terms each (24 bits).  With up to four query heads the terms are columns of their own (kSpread): column 4 r + x holds
+// term x of head r, the scores of four columns are added up, and each multiplies its own term of the weight.  A third of
+// the matrix instructions and half the work of splitting: 1,325 tokens of 12 heads of d64 over 11 pages each 115 -> 95 us.
 //
 // A wavefront loads its next page while it works on one; the wavefronts of a workgroup take every kWaves-th page and are
 // joined in LDS.  Long histories of few units are cut into equal runs of pages, a workgroup each, whose partial results a
@@ -93,8 +93,9 @@ struct Values {
 
 // One head's part of a page as a buffer: no address arithmetic per lane but a fixed offset, and an empty buffer's loads
 // touch no memory, so that the loop below needs no branch around its last loads.
-// Codes are loaded past the caches (kNt): histories of a decode step are read once (32 of them up to 32K tokens: 67 us
-// cached, 60 so), and prompts, whose units share pages, take the same time either way.
+// Codes are loaded past the caches (kNt): histories of a decode step are read once (400 of 32 pages: 91 us cached, 83 so;
+// 64 of 31 listed pages 17.9 and 16.6; 32 of 128 pages on average 61 either way), and prompts, whose units share pages, take
+// the same time either way.
 constexpr int kNt = 2;
 template <int D>
 __device__ __forceinline__ void load_codes(buf_rsrc r, uint32_t offset, uint32_t (&w)[D / 32]) {
@@ -691,20 +692,20 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
     }
     const int64_t units = static_cast<int64_t>((n_tokens + c.tokens - 1) / c.tokens) * plan.p.n_kv_heads;
     c.run = static_cast<int>(entries);
-    // workgroups that the device holds at once or a few more (decode of 32 histories up to 32K, 4 heads of d128: 60 us with 4
-    // a CU, 66-70 with 2, 3 or 6; 512 tokens of a 16K prompt in two tiles: 171 us with 2, 186 with 4)
+    // workgroups that the device holds at once or a few more (decode of 32 histories up to 32K, 4 heads of d128: 61 us with 4
+    // a CU, 68-73 with 2, 3 or 6; 512 tokens of a 16K prompt in two tiles: 198 us with 2, 216 with 4)
     const int64_t want = (c.tiles == 2 ? 2 : 4) * static_cast<int64_t>(plan.n_cu);
     // A history is split where the join costs less than the pages that a workgroup would take one after another: over 64
     // pages, and from fewer where the units leave half of the device idle. 4 heads of d128, split and whole, in us: 1
-    // sequence of 20 pages 8.5 and 9.1, of 32 8.8 and 11.9, of 64 9.1 and 18.1; 16 of 20 10.6 and 10.1, of 32 11.2 and
-    // 12.8; 32 of 32 13.8 and 13.8, of 64 18.8 and 21.8. Tokens of one sequence in two tiles: 4 at 20 pages 16.2 and 20.1,
-    // 64 at 20 pages 20.8 and 20.6, at 32 22.0 and 24.5; 128 at 32 29.6 and 25.1, at 60 34.0 and 33.9.
+    // sequence of 20 pages 8.8 and 9.9, of 32 9.0 and 13.4, of 64 9.3 and 20.5; 16 of 20 11.2 and 10.8, of 32 11.5 and
+    // 14.0; 32 of 32 14.3 and 14.8, of 64 20.1 and 23.4. Tokens of one sequence in two tiles: 4 at 20 pages 18.0 and 23.6,
+    // 64 at 20 pages 23.0 and 23.9, at 32 24.9 and 29.2; 128 at 32 33.5 and 29.4, at 60 38.0 and 40.9.
     const int64_t whole = 2 * units > plan.n_cu ? 64 : 16 + units / 8;
     if (entries > whole && units < want) {
         // A run is 16 pages or more where the device is filled: a part is written and read again. Below that it is the run
         // that gives each compute unit a workgroup, of two tiles every other one, 4 pages at the least (1 sequence of 64
-        // pages: 9.1 us in runs of 4, 10.0 of 8, 11.4 of 16; 8 sequences: 12.3, 11.1, 12.4; 32 tokens in two tiles at 100
-        // pages: 26.1 in runs of 13, 23.0 of 16).
+        // pages: 9.3 us in runs of 4, 10.3 of 8, 12.0 of 16; 8 sequences: 12.7, 11.6, 13.0; 32 tokens in two tiles at 100
+        // pages: 29.7 in runs of 7, 25.3 of 16).
         const int64_t fill = std::max<int64_t>(1, plan.n_cu / (units * c.tiles));
         const int64_t least = std::clamp<int64_t>((entries + fill - 1) / fill, 4, 16);
         const int64_t run = std::max(least, (units * entries + want - 1) / want);
@@ -720,10 +721,10 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
             c.bytes += counts + splits * split_bytes;
         }
     }
-    // A workgroup of 8 wavefronts where a compute unit has one workgroup only (1 sequence of 64 pages, whole: 17.4 us, 18.9
-    // with 4; 64 sequences of 31 listed pages: 15.1 and 15.7; at 400 units of 32 pages 27.4 and 23.4). One wavefront, which
-    // joins nothing, from 24 a compute unit on (16K units of 3 fp32 heads of d64: 130 us, 165 with 4; 6.4K units of bf16
-    // d128: 177 either way; at 1,600 units 58 and 51).
+    // A workgroup of 8 wavefronts where a compute unit has one workgroup only (16 sequences of 20 pages, 4 heads of d128:
+    // 10.8 us, 11.8 with 4; 64 of 31 listed pages: 16.6 and 17.4; 100 of 32 pages 30.2 and 25.3). One wavefront, which joins
+    // nothing, from 24 a compute unit on (16K units of an fp32 head of d64: 95 us, 119 with 4; 6.4K units of 8 bf16 heads of
+    // d128 over 10 pages: 112 and 126; at 1.6K units 31 and 27).
     if (c.tiles == 1 && units * c.splits <= plan.n_cu) c.waves = 8;
     if (c.tiles == 1 && c.splits == 1 && units >= 24 * plan.n_cu) c.waves = 1;
     return c;
