@@ -763,15 +763,15 @@ hipError_t launch_attend_tokens(const hga_plan& plan, const PoolView& pool, cons
     const auto go = [&](auto zero, auto dim) {
         using T = decltype(zero);
         constexpr int D = decltype(dim)::value;
-        constexpr int kTwo = sizeof(T) == 4 && D == 128 ? 1 : 2;
         constexpr bool kF32 = sizeof(T) == 4;
-        const auto spread = c.waves == 8 ? run<T, D, 1, 8, false, kF32>
-                            : c.waves == 1 ? run<T, D, 1, 1, false, kF32> : run<T, D, 1, 4, false, kF32>;
-        const auto f = kF32 && a.ratio <= 4 && c.tokens == 1 ? spread : c.tokens > 1 ? (c.tiles == 2 ? run<T, D, kTwo, 4, true>
-                                       : c.waves == 8 ? run<T, D, 1, 8, true>
-                                       : c.waves == 1 ? run<T, D, 1, 1, true> : run<T, D, 1, 4, true>)
-                                    : c.waves == 8 ? run<T, D, 1, 8, false>
-                                    : c.waves == 1 ? run<T, D, 1, 1, false> : run<T, D, 1, 4, false>;
+        constexpr int kTwo = kF32 && D == 128 ? 1 : 2;  // (cut_call gives those one tile)
+        const auto by_waves = [&](auto one, auto four, auto eight) { return c.waves == 1 ? one : c.waves == 8 ? eight : four; };
+        const auto f = c.tokens > 1 && c.tiles == 2 ? run<T, D, kTwo, 4, true>
+                       : c.tokens > 1
+                           ? by_waves(run<T, D, 1, 1, true>, run<T, D, 1, 4, true>, run<T, D, 1, 8, true>)
+                       : kF32 && a.ratio <= 4
+                           ? by_waves(run<T, D, 1, 1, false, kF32>, run<T, D, 1, 4, false, kF32>, run<T, D, 1, 8, false, kF32>)
+                           : by_waves(run<T, D, 1, 1, false>, run<T, D, 1, 4, false>, run<T, D, 1, 8, false>);
         return f(plan, pool, tok, a, q, q_stride, out, c.grid_units, stream);
     };
     const bool f32 = plan.p.dtype == HGA_F32;
