@@ -416,8 +416,10 @@ def _prepare_own(st):
         st["pool"] = hga.Pool(plan, pages=st["pages"])
         st["batch"] = hga.TokenBatch(st["seq"], st["pos"], st["table"])
     if c["do"] == "shared":
+        # (with the longest shared and unshared parts, as a cache's bookkeeping knows them)
         st["prefixes"] = hga.Prefixes(st["order"], st["begin"], st["shared"],
-                                      max(p for _, p, _, _ in _lens(c)))
+                                      max(p for _, p, _, _ in _lens(c)),
+                                      max(-(-x // PAGE) - p for _, p, x, _ in _lens(c)))
         nbytes = hga.hga_attend_shared_workspace(plan, st["batch"], st["prefixes"])
     elif c["do"] == "weigh":
         nbytes = hga.hga_weigh_pages_workspace(plan, st["batch"], st.get("list"))
