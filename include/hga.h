@@ -741,6 +741,118 @@ hga_status hga_attend_tokens(const hga_plan* plan, const hga_pool* pool, int32_t
 hga_status hga_copy_pages(const hga_plan* plan, const hga_pool* pool, const int32_t* src,
                           const int32_t* dst, int32_t n, void* stream);
 
+/* ---- Shared prefixes --------------------------------------------------------
+ *
+ * Sequences that go on from one prompt (hga_copy_pages and the page table make
+ * them) share its pages.  A call that is told so reads each shared page once
+ * for all of its tokens.
+ *
+ * Slot i of the call is token order[i], a permutation of the tokens.  Slots
+ * [group_begin[g], group_begin[g + 1]) are the tokens of group g, whose
+ * sequences' first group_pages[g] table entries are equal (which of their rows
+ * is read is not said); group_begin ascends.  Slots before group_begin[0] and
+ * from group_begin[n_groups] on share nothing.  A token may lie inside its
+ * group's pages: it sees them up to its position.
+ *   shared_hint, own_hint  the largest of group_pages, and the most pages that a
+ *               token has behind its group's, as far as the host knows; 0: it
+ *               does not.  They say how the work is cut: results are right, up
+ *               to the order of sums, whatever they are (a captured call keeps
+ *               them).
+ * What is read of the device arrays is checked by the kernels: words that are
+ * none of this lead to results of any value, never outside the call's arrays. */
+typedef struct {
+    const int32_t* order;
+    const int32_t* group_begin;
+    const int32_t* group_pages;
+    int32_t n_groups;
+    int32_t shared_hint;
+    int32_t own_hint;
+} hga_prefixes;
+
+/* Bytes hga_attend_shared makes use of at most, or a negative hga_status.  Host
+ * only. */
+int64_t hga_attend_shared_workspace(const hga_plan* plan, int32_t n_tokens, int32_t n_seqs,
+                                    int32_t max_pages, int32_t n_groups, int32_t shared_hint,
+                                    int32_t own_hint);
+
+/* hga_attend_tokens over whole histories, each group's shared pages read once:
+ * out and lse are what that call writes, up to the order of sums.  Arguments,
+ * requirements and errors as there, without lists;
+ *   workspace   hga_attend_shared_workspace bytes; with fewer the work is cut
+ *               into fewer runs, and below a partial result each of the
+ *               groups' and the tokens' own pages nothing is shared (NULL and
+ *               0 are allowed); calls that overlap in time need one each.  Its
+ *               size decides the order of sums, its contents nothing.
+ * HGA_EUNSUPPORTED above 2^20 groups or 2^30 query rows. */
+hga_status hga_attend_shared(const hga_plan* plan, const hga_pool* pool, int32_t layer,
+                             const hga_tokens* tokens, const hga_prefixes* prefixes, const void* q,
+                             int64_t q_stride, void* out, float* lse, void* workspace,
+                             int64_t workspace_bytes, void* stream);
+
+/* ---- Eviction by attention weight -------------------------------------------
+ *
+ * A cache that has outgrown its pool gives up the pages that attention made
+ * least use of: hga_weigh_pages sums up what each page got, token after token,
+ * hga_choose_evictions names those to drop, and their table entries then mark
+ * absent pages. */
+
+/* Bytes of workspace hga_weigh_pages makes use of (n_list 0: every chunk), or a
+ * negative hga_status.  Host only. */
+int64_t hga_weigh_pages_workspace(const hga_plan* plan, int32_t n_tokens, int32_t n_seqs,
+                                  int32_t max_pages, int32_t n_list);
+
+/* What each page of each sequence gets of the attention of the call's tokens:
+ *   weights[s][h][c] = prev[s][h][c] + sum of exp(q . k / sqrt(head_dim) - lse)
+ * over the tokens of sequence s, the query heads of KV head h and the rows, as
+ * stored, of chunk c at positions up to the token's -- with the lse of
+ * hga_attend_tokens or hga_attend_shared for the same rows their softmax weights,
+ * which come to the number of query heads for each token and KV head.
+ *   q           as for the attention
+ *   lse         fp32 [n_tokens][n_q_heads]; a head whose lse is infinite adds
+ *               nothing
+ *   chunk_list  the attention's lists, or NULL with n_list 0: every chunk up to
+ *               the token's own.  Entries count as there (one that stands twice
+ *               counts twice).
+ *   prev        fp32 [n_seqs][n_kv_heads][max_pages], or NULL: zeros; may be
+ *               weights itself
+ *   weights     as prev: every entry is written
+ *   workspace   hga_weigh_pages_workspace bytes, or NULL and 0 (a call of many
+ *               tokens of few pages then takes longer); calls that overlap in
+ *               time need one each.  Its size decides the order of sums.
+ * Sums are held in fp32 and do not depend on anything that runs beside them. */
+hga_status hga_weigh_pages(const hga_plan* plan, const hga_pool* pool, int32_t layer,
+                           const hga_tokens* tokens, const void* q, int64_t q_stride,
+                           const float* lse, const int32_t* chunk_list, int32_t n_list,
+                           const float* prev, float* weights, void* workspace,
+                           int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace hga_choose_evictions needs, or a negative hga_status.  Host
+ * only. */
+int64_t hga_choose_evictions_workspace(const hga_plan* plan, int32_t n_seqs, int32_t max_pages);
+
+/* For each sequence, the chunks to evict so that it holds at most budget[s]
+ * pages: of the middle chunks of its last token (those that routing chooses
+ * from: the first keep_first, the window and the last chunk itself stay) the
+ * present ones with the least weight, summed over the KV heads in 64 bits in
+ * their order; of equal ones the lowest chunk; one that is not a number counts
+ * as the least.  As many as the sequence has pages above its budget, but no more
+ * than there are such chunks and than n_evict.
+ *   page_table  int32 [n_seqs][max_pages]; ids in [0, n_ids) are pages (n_ids =
+ *               the pool's n_pages + n_cold)
+ *   seq_len     int32 [n_seqs]: tokens of the sequence; one of 0 or fewer, or of
+ *               more than max_pages * 64, gets an empty list
+ *   weights     fp32 [n_seqs][n_kv_heads][max_pages]
+ *   budget      int32 [n_seqs]
+ *   evicted     int32 out [n_seqs][n_evict], ascending, padded with -1
+ *   workspace   hga_choose_evictions_workspace bytes; calls that overlap in time
+ *               need one each
+ * Nothing else is changed: the table is the caller's. */
+hga_status hga_choose_evictions(const hga_plan* plan, const int32_t* page_table, int32_t n_seqs,
+                                int32_t max_pages, int32_t n_ids, const int32_t* seq_len,
+                                const float* weights, const int32_t* budget, int32_t* evicted,
+                                int32_t n_evict, void* workspace, int64_t workspace_bytes,
+                                void* stream);
+
 /* Static description of a status code (never NULL). */
 const char* hga_status_string(int32_t status);
 

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "hga_internal.hpp"
+#include "prefixes.hpp"
 #include "tokens.hpp"
 
 namespace hga {
@@ -38,5 +39,25 @@ hipError_t launch_attend_tokens(const hga_plan& plan, const PoolView& pool, cons
                                 const void* q, int64_t q_stride, const int32_t* list, int n_list,
                                 void* out, float* lse, void* ws, int64_t ws_bytes,
                                 hipStream_t stream);
+
+// Attention over prefixes that sequences share, the bytes its workspace may
+// take (must: the fewest with which anything is shared), the pages' attention
+// weight, and the choice of pages to evict.
+int64_t attend_shared_bytes(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages,
+                            int n_groups, int shared_hint, int own_hint, bool must);
+hipError_t launch_attend_shared(const hga_plan& plan, const PoolView& pool, const TokensView& tok,
+                                const PrefixView& prefixes, int shared_hint, int own_hint,
+                                const void* q, int64_t q_stride, void* out, float* lse, void* ws,
+                                int64_t ws_bytes, hipStream_t stream);
+int64_t weigh_pages_bytes(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int n_list);
+hipError_t launch_weigh_pages(const hga_plan& plan, const PoolView& pool, const TokensView& tok,
+                              const void* q, int64_t q_stride, const float* lse, const int32_t* list,
+                              int n_list, const float* prev, float* weights, void* ws,
+                              int64_t ws_bytes, hipStream_t stream);
+int64_t choose_evictions_bytes(int n_seqs, int max_pages);
+hipError_t launch_choose_evictions(const hga_plan& plan, const int32_t* table, int n_seqs,
+                                   int max_pages, int n_ids, const int32_t* seq_len,
+                                   const float* weights, const int32_t* budget, int32_t* evicted,
+                                   int n_evict, void* ws, int64_t ws_bytes, hipStream_t stream);
 
 }  // namespace hga

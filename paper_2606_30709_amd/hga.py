@@ -26,6 +26,8 @@ __all__ = [
     "Pool", "TokenBatch", "hga_page_bytes", "hga_token_list_size", "hga_cache_append",
     "hga_cache_read", "hga_route_tokens", "hga_route_tokens_workspace", "hga_attend_tokens",
     "hga_attend_tokens_workspace", "hga_copy_pages",
+    "Prefixes", "hga_attend_shared", "hga_attend_shared_workspace", "hga_weigh_pages",
+    "hga_weigh_pages_workspace", "hga_choose_evictions", "hga_choose_evictions_workspace",
 ]
 
 F32, BF16 = 0, 1
@@ -43,6 +45,8 @@ EXPORTED_SYMBOLS = (
     "hga_page_bytes", "hga_token_list_size", "hga_cache_append", "hga_cache_read",
     "hga_route_tokens", "hga_route_tokens_workspace", "hga_attend_tokens",
     "hga_attend_tokens_workspace", "hga_copy_pages",
+    "hga_attend_shared", "hga_attend_shared_workspace", "hga_weigh_pages",
+    "hga_weigh_pages_workspace", "hga_choose_evictions", "hga_choose_evictions_workspace",
 )
 
 
@@ -69,6 +73,14 @@ class HgaPool(ctypes.Structure):
     _fields_ = [
         ("pages", ctypes.c_void_p), ("cold", ctypes.c_void_p), ("page_sum", ctypes.c_void_p),
         ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_cold", ctypes.c_int32),
+    ]
+
+
+class HgaPrefixes(ctypes.Structure):
+    _fields_ = [
+        ("order", ctypes.c_void_p), ("group_begin", ctypes.c_void_p),
+        ("group_pages", ctypes.c_void_p), ("n_groups", ctypes.c_int32),
+        ("shared_hint", ctypes.c_int32), ("own_hint", ctypes.c_int32),
     ]
 
 
@@ -144,6 +156,14 @@ def library() -> ctypes.CDLL:
             "hga_attend_tokens": ([vp, pool_p, i32, tok_p, vp, i64, vp, i32, vp, vp, vp, i64, vp],
                                   i32),
             "hga_copy_pages": ([vp, pool_p, vp, vp, i32, vp], i32),
+            "hga_attend_shared_workspace": ([vp, i32, i32, i32, i32, i32, i32], i64),
+            "hga_attend_shared": ([vp, pool_p, i32, tok_p, ctypes.POINTER(HgaPrefixes), vp, i64, vp,
+                                   vp, vp, i64, vp], i32),
+            "hga_weigh_pages_workspace": ([vp, i32, i32, i32, i32], i64),
+            "hga_weigh_pages": ([vp, pool_p, i32, tok_p, vp, i64, vp, vp, i32, vp, vp, vp, i64, vp],
+                                i32),
+            "hga_choose_evictions_workspace": ([vp, i32, i32], i64),
+            "hga_choose_evictions": ([vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, i64, vp], i32),
         }
         for name, (args, res) in more.items():
             fn = getattr(lib, name)
@@ -551,11 +571,15 @@ def _space(workspace, device):
 def _on(pool, stream):
     """The stream to launch on: given, or the current one of the pool's device,
     which must be the current device."""
-    if pool.index != torch.cuda.current_device():
-        _require(False, f"the pool is on {pool.device}, the current device is "
+    return _on_device(pool.index, "the pool", stream)
+
+
+def _on_device(index, what, stream):
+    if index != torch.cuda.current_device():
+        _require(False, f"{what} is on cuda:{index}, the current device is "
                         f"{torch.cuda.current_device()}")
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(pool.index)
+        return torch._C._cuda_getCurrentRawStream(index)
     return _stream(stream)
 
 
@@ -723,3 +747,113 @@ def hga_copy_pages(plan: Plan, pool: Pool, src, dst, stream=None):
     _expect(dst, "dst", torch.int32, (src.numel(),), pool.device)
     _check(library().hga_copy_pages(plan.handle, ctypes.byref(pool.struct), _ptr(src), _ptr(dst),
                                     src.shape[0], _on(pool, stream)))
+
+
+# ------------------------------------------------------------- shared prefixes ---
+
+class Prefixes:
+    """Which tokens of a batch share leading pages: slot i is token ``order[i]``
+    (int32 [n_tokens], a permutation), slots ``group_begin[g]`` to
+    ``group_begin[g + 1]`` (int32 [n_groups + 1]) are those of group g, whose
+    sequences have their first ``group_pages[g]`` pages (int32 [n_groups]) in
+    common.  ``shared_hint`` and ``own_hint``: the most pages of a group, and of
+    a token behind its group's, where they are known.  The tensors are used in
+    place: their contents may change between calls."""
+
+    def __init__(self, order, group_begin, group_pages, shared_hint: int = 0, own_hint: int = 0):
+        dev = order.device
+        _expect(order, "order", torch.int32, (None,), dev)
+        _expect(group_pages, "group_pages", torch.int32, (None,), dev)
+        _expect(group_begin, "group_begin", torch.int32, (group_pages.shape[0] + 1,), dev)
+        _require(order.is_cuda, "order must be on a GPU")
+        self.order, self.group_begin, self.group_pages = order, group_begin, group_pages
+        self.n_groups, self.shared_hint, self.own_hint = group_pages.shape[0], shared_hint, own_hint
+        self.device = dev
+        self.struct = HgaPrefixes(order.data_ptr(), group_begin.data_ptr(), group_pages.data_ptr(),
+                                  self.n_groups, shared_hint, own_hint)
+
+
+def hga_attend_shared_workspace(plan: Plan, batch: TokenBatch, prefixes: Prefixes) -> int:
+    """Bytes of workspace hga_attend_shared makes use of at most."""
+    return _size(library().hga_attend_shared_workspace(
+        plan.handle, batch.n_tokens, batch.n_seqs, batch.max_pages, prefixes.n_groups,
+        prefixes.shared_hint, prefixes.own_hint))
+
+
+def hga_attend_shared(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, prefixes: Prefixes, q,
+                      out, lse=None, workspace=None, stream=None):
+    """Attention of each token over all of its sequence's pages up to its own
+    position, the pages that a group shares read once for all of its tokens.
+    Arguments as for hga_attend_tokens."""
+    _match(plan, pool, batch)
+    p = plan.params
+    qs = _rows(q, "q", plan, batch.n_tokens, p.n_q_heads, pool.device)
+    _expect(out, "out", plan.torch_dtype, (batch.n_tokens, p.n_q_heads, p.head_dim), pool.device)
+    _expect(prefixes.order, "prefixes.order", torch.int32, (batch.n_tokens,), pool.device)
+    if lse is not None:
+        _expect(lse, "lse", torch.float32, (batch.n_tokens, p.n_q_heads), pool.device)
+    _check(library().hga_attend_shared(
+        plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct),
+        ctypes.byref(prefixes.struct), _ptr(q), qs, _ptr(out), _ptr(lse),
+        *_space(workspace, pool.device), _on(pool, stream)))
+
+
+# ------------------------------------------------ eviction by attention weight ---
+
+def hga_weigh_pages_workspace(plan: Plan, batch: TokenBatch, chunk_list=None) -> int:
+    """Bytes of workspace hga_weigh_pages makes use of (often 0)."""
+    n_list = 0 if chunk_list is None else chunk_list.shape[2]
+    return _size(library().hga_weigh_pages_workspace(
+        plan.handle, batch.n_tokens, batch.n_seqs, batch.max_pages, n_list))
+
+
+def hga_weigh_pages(plan: Plan, pool: Pool, layer: int, batch: TokenBatch, q, lse, weights,
+                    prev=None, chunk_list=None, workspace=None, stream=None):
+    """weights fp32 [n_seqs, n_kv_heads, max_pages] = prev (None: zeros; may be
+    weights itself) and what each page gets of the attention of the batch's
+    tokens, whose queries, lse (fp32 [n_tokens, n_q_heads]) and lists are the
+    attention's."""
+    _match(plan, pool, batch)
+    p = plan.params
+    qs = _rows(q, "q", plan, batch.n_tokens, p.n_q_heads, pool.device)
+    _expect(lse, "lse", torch.float32, (batch.n_tokens, p.n_q_heads), pool.device)
+    shape = (batch.n_seqs, p.n_kv_heads, batch.max_pages)
+    _expect(weights, "weights", torch.float32, shape, pool.device)
+    if prev is not None:
+        _expect(prev, "prev", torch.float32, shape, pool.device)
+    n_list = 0
+    if chunk_list is not None:
+        n_list = chunk_list.shape[-1]
+        _expect(chunk_list, "chunk_list", torch.int32, (batch.n_tokens, p.n_kv_heads, n_list),
+                pool.device)
+        _require(n_list > 0, "chunk_list must hold an entry a token")
+    _check(library().hga_weigh_pages(
+        plan.handle, ctypes.byref(pool.struct), layer, ctypes.byref(batch.struct), _ptr(q), qs,
+        _ptr(lse), _ptr(chunk_list), n_list, _ptr(prev), _ptr(weights),
+        *_space(workspace, pool.device), _on(pool, stream)))
+
+
+def hga_choose_evictions_workspace(plan: Plan, page_table) -> int:
+    """Bytes of workspace hga_choose_evictions needs."""
+    return _size(library().hga_choose_evictions_workspace(plan.handle, *page_table.shape))
+
+
+def hga_choose_evictions(plan: Plan, page_table, n_ids: int, seq_len, weights, budget, evicted,
+                         workspace=None, stream=None):
+    """The chunks of each sequence (page_table int32 [n_seqs, max_pages], seq_len
+    and budget int32 [n_seqs]) to drop so that it holds at most its budget of
+    pages, those with the least of weights fp32 [n_seqs, n_kv_heads, max_pages]
+    first, into evicted int32 [n_seqs, n_evict] (ascending, -1 behind).  Ids
+    [0, n_ids) are the pool's pages (n_pages + n_cold)."""
+    dev = page_table.device
+    _expect(page_table, "page_table", torch.int32, (None, None), dev)
+    _require(page_table.is_cuda, "page_table must be on a GPU")
+    n_seqs, max_pages = page_table.shape
+    _expect(seq_len, "seq_len", torch.int32, (n_seqs,), dev)
+    _expect(budget, "budget", torch.int32, (n_seqs,), dev)
+    _expect(weights, "weights", torch.float32, (n_seqs, plan.params.n_kv_heads, max_pages), dev)
+    _expect(evicted, "evicted", torch.int32, (n_seqs, None), dev)
+    _check(library().hga_choose_evictions(
+        plan.handle, _ptr(page_table), n_seqs, max_pages, n_ids, _ptr(seq_len), _ptr(weights),
+        _ptr(budget), _ptr(evicted), evicted.shape[1], *_space(workspace, dev),
+        _on_device(dev.index, "page_table", stream)))

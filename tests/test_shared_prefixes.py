@@ -1,0 +1,131 @@
+"""Attention of batches that share leading pages against the 64-bit definition
+of attention over each token's own row of the table."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import prefix_util as P
+from tokens_util import Scene, f64
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [("bf16", 128, 4, 8), ("f32", 128, 1, 16), ("bf16", 64, 3, 3), ("f32", 64, 2, 1), ("bf16", 64, 1, 16),
+          ("bf16", 128, 5, 2), ("f32", 128, 2, 5), ("f32", 64, 3, 3), ("bf16", 128, 2, 1), ("bf16", 64, 2, 6)]
+
+
+@pytest.fixture(scope="module")
+def hga():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2606_30709_amd import hga as H
+    H.library()
+    return H
+
+
+def _bits(t):
+    return t.contiguous().view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32)
+
+
+def _same(a, b):
+    return all(torch.equal(_bits(x), _bits(y)) for x, y in zip(a, b))
+
+
+def _samples(hga, dtype, d, kv, ratio, n, pages, tail, seed=0, **kw):
+    """n sequences after one prompt of `pages` pages, of tails 1 to tail."""
+    lens = [64 * pages + 1 + i * (tail - 1) // max(n - 1, 1) for i in range(n)]
+    sc = Scene(hga, dtype, d, kv, ratio, lens=lens, seed=seed, **kw)
+    P.share(sc, [(0, list(range(1, n)), pages)])
+    return sc
+
+
+@pytest.mark.parametrize("dtype,d,kv,ratio", SHAPES)
+def test_groups_of_every_kind(hga, dtype, d, kv, ratio):
+    # groups of rows: 0 with 3, 4, 5; 1 with 6; 7 alone in one; 2, 8, 9 in none
+    lens = (64 * 9 + 5, 700, 130, 64 * 9 + 1, 64 * 9, 64 * 11 + 63, 64 * 10 + 2, 200, 1, 64)
+    sc = Scene(hga, dtype, d, kv, ratio, lens=lens, layers=2, layer=1, seed=1, cold=9)
+    P.share(sc, [(0, [3, 4, 5], 9), (1, [6], 4)])
+    seq = [0, 1, 2, 3, 4, 5, 6, 7, 8, 9, -1, 10, 3, 5, 4]
+    pos = [lens[s] - 1 for s in range(10)] + [3, 0, -1, 10 ** 7, 100]   # idle ones; one inside its prefix
+    batch = sc.batch(seq, pos)
+    q = sc.random(len(seq), sc.hq, d, scale=1.5)
+    group = {0: 0, 3: 0, 4: 0, 5: 0, 1: 2, 6: 2, 7: 3}
+    pages = [9, 5, 4, 3]                                                # group 1 has no token
+    px = P.prefixes(hga, seq, group, pages, sc.rng)
+    got = P.attend(sc, batch, px, q)
+    sc.check_attend(q, got)
+    assert _same(got, P.attend(sc, batch, px, q))
+    nb = hga.hga_attend_shared_workspace(sc.plan, batch, px)
+    for part in (0, 16, nb // 2 // 16 * 16, nb + 4096):
+        sc.check_attend(q, P.attend(sc, batch, px, q, workspace=part))
+    # hints of any value, wrong ones among them
+    for hint, own in ((0, 0), (1, 1), (3, 2), (2 ** 31 - 1, 7)):
+        sc.check_attend(q, P.attend(sc, batch, P.prefixes(hga, seq, group, pages, sc.rng, hint, own), q))
+    # groups that share no page, and no groups
+    sc.check_attend(q, P.attend(sc, batch, P.prefixes(hga, seq, group, [0, 0, 0, -3], sc.rng), q))
+    sc.check_attend(q, P.attend(sc, batch, P.prefixes(hga, seq, {}, [], sc.rng), q))
+    # strided queries
+    wide = torch.zeros(len(seq), sc.hq + 3, d, dtype=q.dtype, device="cuda")
+    wide[:, :sc.hq] = q
+    assert _same(got, P.attend(sc, batch, px, wide[:, :sc.hq]))
+
+
+@pytest.mark.parametrize("dtype,d,kv,ratio", SHAPES)
+@pytest.mark.parametrize("n,pages", [(2, 70), (37, 21), (130, 3)])
+def test_samples_of_one_prompt(hga, dtype, d, kv, ratio, n, pages):
+    sc = _samples(hga, dtype, d, kv, ratio, n, pages, 300, seed=n)
+    seq, pos = sc.rng.permutation(n), None
+    pos = [sc.lens[s] - 1 for s in seq]
+    batch = sc.batch(seq, pos)
+    q = sc.random(n, sc.hq, d)
+    px = P.prefixes(hga, seq, {s: 0 for s in range(n)}, [pages], sc.rng, own_hint=5)
+    got = P.attend(sc, batch, px, q)
+    some = slice(None) if n < 40 else slice(0, 40)
+    sc.check_attend(q, got, tokens=some)
+    assert _same(got, P.attend(sc, batch, px, q))
+
+
+@pytest.mark.parametrize("dtype,d,kv,ratio,new", [("bf16", 128, 2, 8, 40), ("f32", 64, 2, 3, 5), ("bf16", 64, 1, 1, 70),
+                                                  ("f32", 128, 1, 4, 33), ("bf16", 128, 1, 5, 17)])
+def test_drafts_and_questions_after_one_prompt(hga, dtype, d, kv, ratio, new):
+    """Several tokens of each sequence, each up to itself; the tokens of a
+    sequence together and apart, one sequence without a group."""
+    n, pages = 4, 18
+    sc = _samples(hga, dtype, d, kv, ratio, n, pages, 90, seed=new)
+    runs = [(s, max(64 * pages - 3, x - new), x) for s, x in enumerate(sc.lens)]
+    seq = np.concatenate([[s] * (b - a) for s, a, b in runs])
+    pos = np.concatenate([np.arange(a, b) for _, a, b in runs])
+    group = {s: 0 for s in range(n - 1)}
+    for shuffle in (False, True):
+        o = sc.rng.permutation(len(seq)) if shuffle else np.arange(len(seq))
+        batch = sc.batch(seq[o], pos[o])
+        q = sc.random(len(seq), sc.hq, d)
+        px = P.prefixes(hga, seq[o], group, [pages], sc.rng)
+        sc.check_attend(q, P.attend(sc, batch, px, q))
+        # slots in the batch's own order
+        of = np.array([0 if s in group else 1 for s in seq[o]])
+        order = np.argsort(of, kind="stable")
+        px = hga.Prefixes(P.i32(order), P.i32([0, int((of == 0).sum())]), P.i32([pages]), pages, 3)
+        sc.check_attend(q, P.attend(sc, batch, px, q))
+
+
+def test_absent_and_cold_pages(hga):
+    """Pages of a prefix that are absent count for nothing; a whole prefix of
+    them; a token that sees no row at all."""
+    sc = _samples(hga, "bf16", 128, 2, 4, 6, 30, 200, seed=9, cold=25)
+    sc.table[:, 3:17] = [-1, sc.n_ids, 2 ** 31 - 1, -2 ** 31, -5] + [-1] * 9
+    sc.table[5, 30:] = -1
+    seq = list(range(6)) + [2, 5]
+    pos = [n - 1 for n in sc.lens] + [4 * 64 + 9, 64 * 30]
+    batch = sc.batch(seq, pos)
+    q = sc.random(len(seq), sc.hq, 128)
+    px = P.prefixes(hga, seq, {s: 0 for s in range(6)}, [30], sc.rng)
+    sc.check_attend(q, P.attend(sc, batch, px, q))
+    sc.table[:, :30] = -1
+    batch = sc.batch(seq, pos)
+    got = P.attend(sc, batch, px, q)
+    sc.check_attend(q, got)
+    none = [i for i, (s, p) in enumerate(zip(seq, pos)) if s == 5 or p < 64 * 30]
+    assert len(none) == 3 and (f64(got[0])[none] == 0).all() and (f64(got[1])[none] == -np.inf).all()
