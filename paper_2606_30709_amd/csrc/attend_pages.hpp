@@ -76,31 +76,31 @@ struct Values {
 // 64 of 31 listed pages 17.9 and 16.6; 32 of 128 pages on average 61 either way), and prompts, whose units share pages, take
 // the same time either way.
 constexpr int kNt = 2;
-template <int D>
+template <int D, int kAux = kNt>
 __device__ __forceinline__ void load_codes(buf_rsrc r, uint32_t offset, uint32_t (&w)[D / 32]) {
     if constexpr (D == 128) {
-        const vec16 x = __builtin_bit_cast(vec16, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, kNt));
+        const vec16 x = __builtin_bit_cast(vec16, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, kAux));
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = x.w[i];
     } else {
-        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, kNt));
+        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, kAux));
         w[0] = x.x;
         w[1] = x.y;
     }
 }
-template <int D>
+template <int D, int kAux = kNt>
 __device__ __forceinline__ void load_keys(buf_rsrc r, int m, int g, Keys<D>& k) {
     using F = PageFormat<D>;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) load_codes<D>(r, F::key_code(m, g * (D / 4)) + t * F::key_code(16, 0), k.c[t]);
+    for (int t = 0; t < 4; ++t) load_codes<D, kAux>(r, F::key_code(m, g * (D / 4)) + t * F::key_code(16, 0), k.c[t]);
     k.s = static_cast<uint32_t>(buf_load_i32(r, F::key_scale(m, g * (D / 4) / 32)));
 }
-template <int D>
+template <int D, int kAux = kNt>
 __device__ __forceinline__ void load_values(buf_rsrc r, int m, int g, Values<D>& v) {
     using F = PageFormat<D>;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
-        load_codes<D>(r, F::value_code(4 * g, m * F::kLaneDims) + t * (F::value_code(16, 0) - F::kCodes), v.c[t]);
+        load_codes<D, kAux>(r, F::value_code(4 * g, m * F::kLaneDims) + t * (F::value_code(16, 0) - F::kCodes), v.c[t]);
     const vec16 x = buf_load16(r, F::value_scale(4 * g, m * F::kLaneDims / 32));
 #pragma unroll
     for (int t = 0; t < 4; ++t) v.s[t] = x.w[t];

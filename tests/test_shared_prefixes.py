@@ -55,17 +55,17 @@ def test_groups_of_every_kind(hga, dtype, d, kv, ratio):
     pages = [9, 5, 4, 3]                                                # group 1 has no token
     px = P.prefixes(hga, seq, group, pages, sc.rng)
     got = P.attend(sc, batch, px, q)
-    sc.check_attend(q, got)
+    P.check_attend(sc, q, got)
     assert _same(got, P.attend(sc, batch, px, q))
     nb = hga.hga_attend_shared_workspace(sc.plan, batch, px)
     for part in (0, 16, nb // 2 // 16 * 16, nb + 4096):
-        sc.check_attend(q, P.attend(sc, batch, px, q, workspace=part))
+        P.check_attend(sc, q, P.attend(sc, batch, px, q, workspace=part))
     # hints of any value, wrong ones among them
     for hint, own in ((0, 0), (1, 1), (3, 2), (2 ** 31 - 1, 7)):
-        sc.check_attend(q, P.attend(sc, batch, P.prefixes(hga, seq, group, pages, sc.rng, hint, own), q))
+        P.check_attend(sc, q, P.attend(sc, batch, P.prefixes(hga, seq, group, pages, sc.rng, hint, own), q))
     # groups that share no page, and no groups
-    sc.check_attend(q, P.attend(sc, batch, P.prefixes(hga, seq, group, [0, 0, 0, -3], sc.rng), q))
-    sc.check_attend(q, P.attend(sc, batch, P.prefixes(hga, seq, {}, [], sc.rng), q))
+    P.check_attend(sc, q, P.attend(sc, batch, P.prefixes(hga, seq, group, [0, 0, 0, -3], sc.rng), q))
+    P.check_attend(sc, q, P.attend(sc, batch, P.prefixes(hga, seq, {}, [], sc.rng), q))
     # strided queries
     wide = torch.zeros(len(seq), sc.hq + 3, d, dtype=q.dtype, device="cuda")
     wide[:, :sc.hq] = q
@@ -83,7 +83,7 @@ def test_samples_of_one_prompt(hga, dtype, d, kv, ratio, n, pages):
     px = P.prefixes(hga, seq, {s: 0 for s in range(n)}, [pages], sc.rng, own_hint=5)
     got = P.attend(sc, batch, px, q)
     some = slice(None) if n < 40 else slice(0, 40)
-    sc.check_attend(q, got, tokens=some)
+    P.check_attend(sc, q, got, tokens=some)
     assert _same(got, P.attend(sc, batch, px, q))
 
 
@@ -103,12 +103,12 @@ def test_drafts_and_questions_after_one_prompt(hga, dtype, d, kv, ratio, new):
         batch = sc.batch(seq[o], pos[o])
         q = sc.random(len(seq), sc.hq, d)
         px = P.prefixes(hga, seq[o], group, [pages], sc.rng)
-        sc.check_attend(q, P.attend(sc, batch, px, q))
+        P.check_attend(sc, q, P.attend(sc, batch, px, q))
         # slots in the batch's own order
         of = np.array([0 if s in group else 1 for s in seq[o]])
         order = np.argsort(of, kind="stable")
         px = hga.Prefixes(P.i32(order), P.i32([0, int((of == 0).sum())]), P.i32([pages]), pages, 3)
-        sc.check_attend(q, P.attend(sc, batch, px, q))
+        P.check_attend(sc, q, P.attend(sc, batch, px, q))
 
 
 def test_absent_and_cold_pages(hga):
@@ -122,10 +122,10 @@ def test_absent_and_cold_pages(hga):
     batch = sc.batch(seq, pos)
     q = sc.random(len(seq), sc.hq, 128)
     px = P.prefixes(hga, seq, {s: 0 for s in range(6)}, [30], sc.rng)
-    sc.check_attend(q, P.attend(sc, batch, px, q))
+    P.check_attend(sc, q, P.attend(sc, batch, px, q))
     sc.table[:, :30] = -1
     batch = sc.batch(seq, pos)
     got = P.attend(sc, batch, px, q)
-    sc.check_attend(q, got)
+    P.check_attend(sc, q, got)
     none = [i for i, (s, p) in enumerate(zip(seq, pos)) if s == 5 or p < 64 * 30]
     assert len(none) == 3 and (f64(got[0])[none] == 0).all() and (f64(got[1])[none] == -np.inf).all()
