@@ -94,7 +94,8 @@ hga_status hga_weigh_pages(const hga_plan* plan, const hga_pool* pool, int32_t l
     tv.max_pages = tokens->max_pages;
     const int64_t cells = static_cast<int64_t>(tv.n_seqs) * plan->p.n_kv_heads;
     if (cells == 0 || tv.max_pages == 0) return HGA_OK;
-    if (cells > kMaxUnits) return fail(HGA_EUNSUPPORTED, "n_seqs * n_kv_heads above 2^30 is not supported");
+    if (cells > kMaxUnits || cells * tv.max_pages > kMaxUnits * 256)
+        return fail(HGA_EUNSUPPORTED, "weights of more than 2^38 entries, or 2^30 rows, are not supported");
     HGA_TRY(check_index(weights, "weights"));
     if (prev) HGA_TRY(check_index(prev, "prev"));
     if (tv.n_tokens > 0) {

@@ -144,6 +144,24 @@ def test_chosen_pages(hga, kv, first, last, n):
             assert np.array_equal(got, P.choose(table, 5000, lens, w, budget, most, first, max(last, 1)))
 
 
+@pytest.mark.parametrize("n", [1024, 1025, 4100, 16384, 16385, 40000])
+def test_chosen_pages_of_long_tables(hga, n):
+    """Keys in registers and in the workspace; equal ones in every place."""
+    rng = np.random.default_rng(n)
+    S, kv = 4, 2
+    plan = hga.Plan(batch=1, n_q_heads=kv, n_kv_heads=kv, head_dim=64, keep_first=1, keep_last=3, force_prev=1,
+                    topk_chunks=4, topk_groups=4)
+    table = np.where(rng.random((S, n)) < 0.02, -1, rng.integers(0, 10 ** 6, (S, n))).astype(np.int32)
+    lens = np.array([64 * n, 64 * n - 63, 64 * (n // 2) + 5, 64 * n - 7])
+    w = np.exp(3 * rng.standard_normal((S, kv, n))).astype(np.float32)
+    w[1] = rng.integers(0, 3, (kv, n))     # three values in all
+    w[2] = 0.25                            # one
+    w[3, 0], w[3, 1] = 1e30, rng.random(n)  # sums apart in their last bits, or not at all
+    for budget in ([n // 4] * 4, [n - 20] * 4, [5] * 4, [n // 2, n // 3, 1, 0]):
+        got = P.run_choose(hga, plan, table, 10 ** 6, lens, w, budget, n)
+        assert np.array_equal(got, P.choose(table, 10 ** 6, lens, w, budget, n, 1, 3))
+
+
 def test_weights_that_fp32_sums_cannot_tell_apart(hga):
     n = 400
     plan = hga.Plan(batch=1, n_q_heads=3, n_kv_heads=3, head_dim=64, keep_first=1, keep_last=0, force_prev=1,
