@@ -255,21 +255,24 @@ __device__ __forceinline__ void half_values(int u, const Values<D>& v, const u32
                 acc.o[i][j] = mfma(u32x4{vf[j][0], vf[j][1], vf[j][2], vf[j][3]}, w[i][x], acc.o[i][j]);
 }
 
+// Bit 7 of each byte that is 255.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u; }
+
 // Value blocks of a page that stand for NaN, where some columns see a row and others do not: 0 * NaN would reach those too.
-// They count as some number from here on, and the columns that see them become NaN (the block's dimensions): column
-// 16 i + m sees the page's rows up to seen[i].
+// They count as some number from here on, and the columns that see them are to become NaN (the block's dimensions): column
+// 16 i + m sees the page's rows up to seen[i]; bit i of the result: it does, in the lane's dimensions (a block's:
+// (4 g + x) DL + j, x < 4, j < DL).
 template <int D, int kTiles>
-__device__ __forceinline__ void take_out_nan(Values<D>& v, int m, int g, const int (&seen)[kTiles], Acc<D, kTiles>& acc) {
+__device__ __forceinline__ uint32_t nan_reached(Values<D>& v, int m, int g, const int (&seen)[kTiles]) {
     constexpr int DL = D / 16;
-    const auto bytes_255 = [](uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u; };
     uint32_t any = 0;
 #pragma unroll
-    for (int tt = 0; tt < 4; ++tt) any |= bytes_255(v.s[tt]);
-    if (!__builtin_amdgcn_ballot_w64(any != 0)) return;
-    uint32_t reached = 0;  // bit i: column 16 i + m, in the lane's dimensions (a block's: (4 g + x) DL + j, x < 4, j < DL)
+    for (int tt = 0; tt < 4; ++tt) any |= nan_bytes(v.s[tt]);
+    if (!__builtin_amdgcn_ballot_w64(any != 0)) return 0;
+    uint32_t reached = 0;
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) {
-        const uint32_t is = bytes_255(v.s[tt]);
+        const uint32_t is = nan_bytes(v.s[tt]);
         for (int x = 0; x < 4; ++x) {
             // one lane for a block's: those of its first dimensions
             uint64_t lanes = __builtin_amdgcn_ballot_w64((is >> (8 * x) & 0x80u) != 0 && m * DL % 32 == 0);
@@ -282,11 +285,19 @@ __device__ __forceinline__ void take_out_nan(Values<D>& v, int m, int g, const i
         }
         v.s[tt] ^= is;  // 127, a scale of 1
     }
+    return reached;
+}
+template <int D, int kTiles>
+__device__ __forceinline__ void set_nan(uint32_t reached, Acc<D, kTiles>& acc) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
         if (reached >> i & 1)
 #pragma unroll
-            for (int j = 0; j < DL; ++j) acc.o[i][j] = f32x4{NAN, NAN, NAN, NAN};
+            for (int j = 0; j < D / 16; ++j) acc.o[i][j] = f32x4{NAN, NAN, NAN, NAN};
+}
+template <int D, int kTiles>
+__device__ __forceinline__ void take_out_nan(Values<D>& v, int m, int g, const int (&seen)[kTiles], Acc<D, kTiles>& acc) {
+    set_nan<D, kTiles>(nan_reached<D, kTiles>(v, m, g, seen), acc);
 }
 
 // The weight of a partial result with reference m under the reference `base`.  One without a reference has seen nothing

@@ -16,13 +16,6 @@
 namespace hga {
 namespace {
 
-// How a call is cut: slots of a unit, pages of a run and runs of a unit at most, units; [0] the groups' pages, [1] the
-// tokens' own.
-struct Cut {
-    int slots[2], run[2], most[2], units[2];
-    int64_t counts, part, part_ml, bytes;  // the workspace, in bytes from its start
-};
-
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -45,12 +38,11 @@ __device__ __forceinline__ uint32_t decode2h(uint32_t codes, float scale) {
 }
 
 // Whether every scale of a page's values has an exponent byte of 109 .. 140.
-template <int D>
-__device__ __forceinline__ bool values_fit(const Values<D>& v) {
+__device__ __forceinline__ bool values_fit(const uint32_t (&s)[4]) {
     uint32_t any = 0, all = ~0u;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const uint32_t w = v.s[t] + 0x13131313u;  // 128 .. 159; a byte that carries into the next is out of range itself
+        const uint32_t w = s[t] + 0x13131313u;  // 128 .. 159; a byte that carries into the next is out of range itself
         any |= w;
         all &= w;
     }
@@ -85,12 +77,34 @@ __device__ __forceinline__ void each(std::integer_sequence<int, kAt...>, F f) {
     (f(std::integral_constant<int, kAt>()), ...);
 }
 
-// Weights of half a page and their product with its values: kHalf in f16, else in bf16 of kParts terms a weight.  Two
-// dimensions of the lane's at a time, so that few registers hold decoded values.
-template <int D, bool kHalf, int kParts, int kTiles>
-__device__ __forceinline__ void half_page(int u, const f32x4 (&sc)[kTiles][4], float scale, const Values<D>& v,
-                                          Acc<D, kTiles>& acc) {
-    constexpr int DL = D / 16;
+// The lane's dimensions 2 j and 2 j + 1 of half a page's rows, whose scales are vs, paired by row: what byte kByte of each
+// row's codes holds (kRow: bytes from one row's codes to the next one's in a word).
+template <int D, bool kHalf, int kByte>
+__device__ __forceinline__ void value_pair(const uint32_t (&c0)[D / 32], const uint32_t (&c1)[D / 32], const float (&vs)[2][4],
+                                           u32x4& even, u32x4& odd) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r2 = 0; r2 < 2; ++r2) {
+            const uint32_t* c = b ? c1 : c0;
+            const float s0 = vs[b][2 * r2], s1 = vs[b][2 * r2 + 1];
+            uint32_t lo, hi;
+            if constexpr (D == 128) {
+                lo = kHalf ? decode2h<kByte>(c[2 * r2], s0) : decode2<kByte>(c[2 * r2], s0);
+                hi = kHalf ? decode2h<kByte>(c[2 * r2 + 1], s1) : decode2<kByte>(c[2 * r2 + 1], s1);
+            } else {
+                lo = kHalf ? decode2h<kByte>(c[r2], s0) : decode2<kByte>(c[r2], s0);
+                hi = kHalf ? decode2h<kByte + 2>(c[r2], s1) : decode2<kByte + 2>(c[r2], s1);
+            }
+            even[2 * b + r2] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+            odd[2 * b + r2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+        }
+}
+
+// Weights of half a page and their product with its values: kHalf in f16, else in bf16 of kParts terms a weight.  `values`
+// gives the lane's dimensions 2 j and 2 j + 1 at a time, so that few registers hold decoded values.
+template <int D, bool kHalf, int kParts, int kTiles, typename V>
+__device__ __forceinline__ void half_page(int u, const f32x4 (&sc)[kTiles][4], float scale, V values, Acc<D, kTiles>& acc) {
     u32x4 w[kTiles][kParts];
     if constexpr (kHalf) {
 #pragma unroll
@@ -111,31 +125,10 @@ __device__ __forceinline__ void half_page(int u, const f32x4 (&sc)[kTiles][4], f
     } else {
         half_weights<D, kParts, kTiles>(u, sc, scale, acc, w, nullptr);
     }
-    if constexpr (kTiles > 1) __builtin_amdgcn_sched_barrier(0);  // or the registers do not suffice
-    float vs[2][4];  // scales of the lane's rows
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) vs[b][r] = scale_of(v.s[2 * u + b] >> (8 * r) & 255u);
-    each(std::make_integer_sequence<int, DL / 2>(), [&](auto at) {
+    each(std::make_integer_sequence<int, D / 32>(), [&](auto at) {
         constexpr int j = decltype(at)::value;
         u32x4 even, odd;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r2 = 0; r2 < 2; ++r2) {
-                const uint32_t* c = v.c[2 * u + b];
-                uint32_t lo, hi;
-                if constexpr (DL == 8) {
-                    lo = kHalf ? decode2h<j>(c[2 * r2], vs[b][2 * r2]) : decode2<j>(c[2 * r2], vs[b][2 * r2]);
-                    hi = kHalf ? decode2h<j>(c[2 * r2 + 1], vs[b][2 * r2 + 1]) : decode2<j>(c[2 * r2 + 1], vs[b][2 * r2 + 1]);
-                } else {
-                    lo = kHalf ? decode2h<j>(c[r2], vs[b][2 * r2]) : decode2<j>(c[r2], vs[b][2 * r2]);
-                    hi = kHalf ? decode2h<j + 2>(c[r2], vs[b][2 * r2 + 1]) : decode2<j + 2>(c[r2], vs[b][2 * r2 + 1]);
-                }
-                even[2 * b + r2] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
-                odd[2 * b + r2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-            }
+        values(at, even, odd);
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
 #pragma unroll
@@ -143,30 +136,51 @@ __device__ __forceinline__ void half_page(int u, const f32x4 (&sc)[kTiles][4], f
                 acc.o[i][2 * j] = kHalf ? mfma_f16(even, w[i][x], acc.o[i][2 * j]) : mfma(even, w[i][x], acc.o[i][2 * j]);
                 acc.o[i][2 * j + 1] = kHalf ? mfma_f16(odd, w[i][x], acc.o[i][2 * j + 1]) : mfma(odd, w[i][x], acc.o[i][2 * j + 1]);
             }
-        if constexpr (!kHalf) __builtin_amdgcn_sched_barrier(0);
     });
 }
+
+// The scales of a lane's eight rows of half a page.
+__device__ __forceinline__ void row_scales(uint32_t w0, uint32_t w1, float (&vs)[2][4]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        vs[0][r] = scale_of(w0 >> (8 * r) & 255u);
+        vs[1][r] = scale_of(w1 >> (8 * r) & 255u);
+    }
+}
+// Rows of a lane from `rows` on get a scale of 1: they may hold anything.
+__device__ __forceinline__ void cut_rows(uint32_t (&s)[4], int g, int rows) {
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (16 * tt + 4 * g + x >= rows) s[tt] = (s[tt] & ~(255u << (8 * x))) | 127u << (8 * x);
+}
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 struct SharedArgs {
     int ratio;
     int slots[2], run[2], most[2], units[2];
+    bool alone;       // a wavefront by itself takes a unit of own pages, not a workgroup
     float* lse;
     int32_t* counts;  // [slot][2]: runs of its group's pages, of its own
     float* part;      // their results [run][slot][query head][d], not divided by the sum; the groups' runs first
     float* part_ml;   // ... and [run][slot][query head][2]: reference, sum
 };
 
-// The group of a slot: of the groups that begin at or before it the last, if the slot is inside it; -1: none.
+// The group of a slot (each lane its own): of the groups that begin at or before it the last, if the slot is inside it;
+// -1: none.
 __device__ __forceinline__ int group_of(const PrefixView& px, int n_tokens, int slot) {
-    const int lane = threadIdx.x & 63;
-    int n = 0;
-    for (int g0 = 0; g0 <= px.n_groups; g0 += 64) {
-        const int g = g0 + lane;
-        const bool before = px.n_groups > 0 && g <= px.n_groups && px.begin[g] <= slot;
-        n += __popcll(__builtin_amdgcn_ballot_w64(before));
+    int lo = 0, hi = px.n_groups > 0 ? px.n_groups + 1 : 0;  // begin[0, lo) <= slot < begin[hi, ...)
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (px.begin[mid] <= slot)
+            lo = mid + 1;
+        else
+            hi = mid;
     }
-    if (n == 0 || n > px.n_groups) return -1;
-    return slot >= px.first(n - 1, n_tokens) && slot < px.end(n - 1, n_tokens) ? n - 1 : -1;
+    if (lo == 0 || lo > px.n_groups) return -1;
+    return slot >= px.first(lo - 1, n_tokens) && slot < px.end(lo - 1, n_tokens) ? lo - 1 : -1;
 }
 
 // Slots [a, b) of unit `unit` of the groups, and its group; g -1: there is no such unit.
@@ -192,44 +206,63 @@ __device__ __forceinline__ GroupUnit group_unit(const PrefixView& px, int n_toke
     return GroupUnit{-1, 0, 0};
 }
 
-// Slots of one group (over its shared pages, [0, shared)) or of one sequence (over its own, from `shared` on): their
-// queries against run `split` of the pages.
-template <typename T, int D, int kTiles, int kWaves, bool kOwn>
-__device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensView& tok, const PrefixView& px,
-                                             const SharedArgs& a, const T* __restrict__ q, int64_t q_stride,
-                                             T* __restrict__ out, float* smem, int h, int at, int n_slots, int shared,
-                                             int split) {
-    using F = PageFormat<D>;
-    constexpr int kThreads = 64 * kWaves;
-    constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;       // of a query
-    constexpr int DL = F::kLaneDims;
-    constexpr int kSteps = D / 32;
-    constexpr int kAux = kOwn ? kNt : 0;  // a group's pages are read by its other units too
-    const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(D));  // log2(e) / sqrt(d)
-    float(*s_o)[16 * kTiles][D + 4] = reinterpret_cast<float(*)[16 * kTiles][D + 4]>(smem);
-    float(*s_m)[16 * kTiles] = reinterpret_cast<float(*)[16 * kTiles]>(smem + kWaves * 16 * kTiles * (D + 4));
-    float(*s_l)[16 * kTiles] = s_m + kWaves;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, g = lane >> 4;
-    const int columns = n_slots * a.ratio, heads = pool.n_kv * a.ratio;
+__device__ __forceinline__ void add_scaled(float4& o, float f, const float4& x) {
+    o.x += f * x.x;
+    o.y += f * x.y;
+    o.z += f * x.z;
+    o.w += f * x.w;
+}
+// Four dimensions of a result, o / l.
+__device__ __forceinline__ void store4(float* to, const float4& o, float l) {
+    *reinterpret_cast<float4*>(to) =
+        l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
+}
+__device__ __forceinline__ void store4(bf16_t* to, const float4& o, float l) {
+    *reinterpret_cast<uint2*>(to) =
+        l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack2(o.x / l, o.y / l), pack2(o.z / l, o.w / l));
+}
+// Four dimensions of a row: of the results (whole), or of the partial ones.
+template <typename T, int D>
+__device__ __forceinline__ void put4(const SharedArgs& a, T* out, bool whole, int64_t row, int dim, const float4& o, float top,
+                                     float l) {
+    if (whole) {
+        store4(out + row * D + dim, o, l);
+        if (a.lse && dim == 0) a.lse[row] = natural_lse(top == -INFINITY ? 0.f : top, l);
+    } else {
+        *reinterpret_cast<float4*>(a.part + row * D + dim) = o;
+        if (dim == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * row) = make_float2(top, l);
+    }
+}
 
+// A wavefront's columns: columns c0 + 16 i + m of the slots from `at` on.
+template <typename T, int D, int kTiles>
+struct Columns {
+    static constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;  // of a query
+    u32x4 qf[kTiles][kTerms][D / 32];
     int pos[kTiles];
-    int s = 0, last = -1, first = INT32_MAX;  // the row of the table, the tokens' largest and smallest positions
-    u32x4 qf[kTiles][kTerms][kSteps];
+    int s, last, first;  // the row of the table, the tokens' largest and smallest positions
+};
+template <typename T, int D, int kTiles>
+__device__ __forceinline__ void load_columns(const PoolView& pool, const TokensView& tok, const PrefixView& px, int ratio,
+                                             const T* q, int64_t q_stride, int h, int at, int c0, int columns, int m, int g,
+                                             Columns<T, D, kTiles>& r) {
+    constexpr int kTerms = Columns<T, D, kTiles>::kTerms;
+    int s = 0, last = -1, first = INT32_MAX;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-        const int c = 16 * i + m;
+        const int c = c0 + 16 * i + m;
         const bool real = c < columns;
-        const int t = real ? px.token(at + c / a.ratio, tok.n_tokens) : -1;
+        const int t = real ? px.token(at + c / ratio, tok.n_tokens) : -1;
         int sc = 0, pc = 0;
         const bool in = t >= 0 && tok.at(t, sc, pc);
-        pos[i] = in ? pc : -1;
-        last = max(last, pos[i]);
+        r.pos[i] = in ? pc : -1;
+        last = max(last, r.pos[i]);
         // columns past the last are no reason to look at rows one by one
-        first = min(first, real ? pos[i] : INT32_MAX);
+        first = min(first, real ? r.pos[i] : INT32_MAX);
         s = in ? max(s, sc) : s;
-        const T* from = q + (in ? t * q_stride : 0) + (static_cast<int64_t>(h) * a.ratio + c % a.ratio) * D + g * (D / 4);
+        const T* from = q + (in ? t * q_stride : 0) + (static_cast<int64_t>(h) * ratio + c % ratio) * D + g * (D / 4);
 #pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) {
+        for (int kk = 0; kk < D / 32; ++kk) {
             float x[8] = {};
             if (in) load8(from + 8 * kk, x);
 #pragma unroll
@@ -237,7 +270,7 @@ __device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensV
                 uint32_t w[kTerms];
                 split2<kTerms>(x[2 * e], x[2 * e + 1], w);
 #pragma unroll
-                for (int y = 0; y < kTerms; ++y) qf[i][y][kk][e] = w[y];
+                for (int y = 0; y < kTerms; ++y) r.qf[i][y][kk][e] = w[y];
             }
         }
     }
@@ -247,38 +280,104 @@ __device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensV
         first = min(first, __shfl_xor(first, x));
         s = max(s, __shfl_xor(s, x));
     }
-    s = __builtin_amdgcn_readfirstlane(s);
-    first = __builtin_amdgcn_readfirstlane(first);
-    last = __builtin_amdgcn_readfirstlane(last);
-    const int n_all = !kOwn ? shared : last < 0 ? 0 : last / kPageRows + 1 - shared;
-    bool whole = false;  // no other workgroup has a part of it
-    if constexpr (kOwn) {
-        const int parts = runs_of(n_all, a.run[1], a.most[1]);
-        const int parts_group = last >= 0 ? runs_of(shared, a.run[0], a.most[0]) : 0;
-        if (split == 0 && h == 0 && tid < n_slots) {
-            a.counts[2 * (at + tid)] = parts_group;
-            a.counts[2 * (at + tid) + 1] = parts;
-        }
-        if (split >= (parts_group == 0 ? max(parts, 1) : parts)) return;
-        whole = parts_group == 0 && parts <= 1;
-    }
-    PageRun run = page_run(split, n_all, a.run[kOwn], a.most[kOwn]);
-    if (kOwn) run = PageRun{run.a + shared, run.b + shared};
-    const int to = last < 0 ? run.a : min(run.b, last / kPageRows + 1);
-
-    Acc<D, kTiles> acc;
+    r.s = __builtin_amdgcn_readfirstlane(s);
+    r.first = __builtin_amdgcn_readfirstlane(first);
+    r.last = __builtin_amdgcn_readfirstlane(last);
+}
+template <int D, int kTiles>
+__device__ __forceinline__ void clear(Acc<D, kTiles>& acc) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
         acc.m[i] = -INFINITY;
         acc.l[i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < DL; ++j) acc.o[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < D / 16; ++j) acc.o[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    for (int e0 = run.a + wave; e0 < to; e0 += 64 * kWaves) {
+}
+// Scores of rows that a column does not see (`seen`: the last it sees) to -infinity.
+template <int kTiles>
+__device__ __forceinline__ void hide_rows(const int (&seen)[kTiles], int g, f32x4 (&sc)[kTiles][4]) {
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+                if (16 * tt + 4 * g + x > seen[i]) sc[i][tt][x] = -INFINITY;
+}
+// A bf16 call's page in f16 if its values allow that, in two bf16 terms if not; an fp32 call's in three.
+template <typename T, typename F>
+__device__ __forceinline__ void by_terms(bool fit, F f) {
+    if constexpr (sizeof(T) == 4)
+        f(std::false_type(), std::integral_constant<int, 3>());
+    else if (__builtin_expect(fit, 1))
+        f(std::true_type(), std::integral_constant<int, 1>());
+    else
+        f(std::false_type(), std::integral_constant<int, 2>());
+}
+
+// A wavefront's results, from its registers: lane (m, g) of tile i holds column c0 + 16 i + m, dimensions (4 g + x) DL + j.
+template <typename T, int D, int kTiles, typename R>
+__device__ __forceinline__ void put_columns(const SharedArgs& a, T* out, const Acc<D, kTiles>& acc, int c0, int columns, int m,
+                                            int g, R row_of) {
+    constexpr int DL = D / 16;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+        const float l = sum_groups(acc.l[i]);
+        const int c = c0 + 16 * i + m;
+        if (c >= columns) continue;
+        bool whole;
+        const int64_t row = row_of(c, whole);
+        if (row < 0) continue;
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int j = 0; j < DL; j += 4)
+                put4<T, D>(a, out, whole, row, (4 * g + x) * DL + j,
+                           make_float4(acc.o[i][j][x], acc.o[i][j + 1][x], acc.o[i][j + 2][x], acc.o[i][j + 3][x]), acc.m[i], l);
+    }
+}
+
+// Up to 16 columns of one group (over its shared pages, [0, shared)) or of one sequence (over its own, from `shared` on):
+// their queries against run `split` of the pages, which n_waves wavefronts take in turns and join (n_waves 1: this one by
+// itself, without a barrier).
+template <typename T, int D, bool kOwn, bool kAlone>
+__device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensView& tok, const PrefixView& px,
+                                             const SharedArgs& a, const T* __restrict__ q, int64_t q_stride,
+                                             T* __restrict__ out, float* smem, int h, int at, int n_slots, int shared,
+                                             int split) {
+    using F = PageFormat<D>;
+    constexpr int kTerms = Columns<T, D, 1>::kTerms, DL = D / 16, kTeam = kAlone ? 1 : kWaves;
+    constexpr int kAux = kOwn ? kNt : 0;  // a group's pages are read by its other units too
+    const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(D));  // log2(e) / sqrt(d)
+    const int tid = threadIdx.x, wave = kAlone ? 0 : tid >> 6, lane = tid & 63, m = lane & 15, g = lane >> 4;
+    const int columns = n_slots * a.ratio, heads = pool.n_kv * a.ratio;
+
+    Columns<T, D, 1> col;
+    load_columns<T, D, 1>(pool, tok, px, a.ratio, q, q_stride, h, at, 0, columns, m, g, col);
+    const int last = col.last;
+    const int n_all = !kOwn ? shared : last < 0 ? 0 : last / kPageRows + 1 - shared;
+    bool whole = false;  // there is no other part of it
+    if constexpr (kOwn) {
+        const int parts = runs_of(n_all, a.run[1], a.most[1]), of_group = last >= 0 ? runs_of(shared, a.run[0], a.most[0]) : 0;
+        if (split == 0 && h == 0 && wave == 0 && lane < n_slots) {
+            a.counts[2 * (at + lane)] = of_group;
+            a.counts[2 * (at + lane) + 1] = parts;
+        }
+        whole = of_group == 0 && parts <= 1;
+        if (split >= (whole ? 1 : parts)) return;
+    }
+    PageRun run = page_run(split, n_all, a.run[kOwn], a.most[kOwn]);
+    if (kOwn) run = PageRun{run.a + shared, run.b + shared};
+    const int to = last < 0 ? run.a : min(run.b, last / kPageRows + 1);
+
+    Acc<D, 1> acc;
+    clear(acc);
+    for (int e0 = run.a + wave; e0 < to; e0 += 64 * kTeam) {
         // the next 64 pages of this wavefront, one a lane
         SeenPage mine{-1, 0};
-        const int chunk = e0 + lane * kWaves;
-        if (chunk < to) mine = seen_page(pool, tok, s, last, chunk);
+        const int chunk = e0 + lane * kTeam;
+        if (chunk < to) mine = seen_page(pool, tok, col.s, last, chunk);
         uint64_t left = __builtin_amdgcn_ballot_w64(mine.rows > 0);
         if (!left) continue;
         int cur = static_cast<int>(__builtin_ctzll(left));
@@ -297,232 +396,478 @@ __device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensV
             const int nxt = left ? static_cast<int>(__builtin_ctzll(left)) : cur;
             const buf_rsrc r = part(nxt, left != 0);
             const int c = __builtin_amdgcn_readlane(chunk, cur);
-            f32x4 sc[kTiles][4];
-            page_scores<D, kTerms, kTiles>(k, qf, sc);
-            if constexpr (kTiles == 1) load_keys<D, kAux>(r, m, g, k);
-            if (__builtin_expect(first < c * kPageRows + kPageRows - 1, 0)) {
+            f32x4 sc[1][4];
+            page_scores<D, kTerms, 1>(k, col.qf, sc);
+            load_keys<D, kAux>(r, m, g, k);
+            if (__builtin_expect(col.first < c * kPageRows + kPageRows - 1, 0)) {
                 __asm__ volatile("");  // a branch: most pages need none of this
-                const int rows = __builtin_amdgcn_readlane(mine.rows, cur);
-#pragma unroll
-                for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int at_row = 16 * tt + 4 * g + x;
-                        if (at_row >= rows) v.s[tt] = (v.s[tt] & ~(255u << (8 * x))) | 127u << (8 * x);
-#pragma unroll
-                        for (int i = 0; i < kTiles; ++i)
-                            if (at_row > pos[i] - c * kPageRows) sc[i][tt][x] = -INFINITY;
-                    }
-                int seen[kTiles];
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i) seen[i] = pos[i] - c * kPageRows;
-                take_out_nan<D, kTiles>(v, m, g, seen, acc);
+                cut_rows(v.s, g, __builtin_amdgcn_readlane(mine.rows, cur));
+                const int seen[1] = {col.pos[0] - c * kPageRows};
+                hide_rows<1>(seen, g, sc);
+                take_out_nan<D, 1>(v, m, g, seen, acc);
             }
-            raise_reference<D, kTiles>(sc, scale, acc);
-            const auto both_halves = [&](auto half, auto terms) {
-                half_page<D, decltype(half)::value, decltype(terms)::value, kTiles>(0, sc, scale, v, acc);
-                if constexpr (kTiles > 1) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    load_keys<D, kAux>(r, m, g, k);
+            raise_reference<D, 1>(sc, scale, acc);
+            by_terms<T>(values_fit(v.s), [&](auto half, auto terms) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float vs[2][4];
+                    row_scales(v.s[2 * u], v.s[2 * u + 1], vs);
+                    half_page<D, decltype(half)::value, decltype(terms)::value, 1>(u, sc, scale, [&](auto j, u32x4& even, u32x4& odd) {
+                        value_pair<D, decltype(half)::value, decltype(j)::value>(v.c[2 * u], v.c[2 * u + 1], vs, even, odd);
+                    }, acc);
                 }
-                half_page<D, decltype(half)::value, decltype(terms)::value, kTiles>(1, sc, scale, v, acc);
-            };
-            if constexpr (sizeof(T) == 4)
-                both_halves(std::false_type(), std::integral_constant<int, 3>());
-            else if (__builtin_expect(values_fit<D>(v), 1))
-                both_halves(std::true_type(), std::integral_constant<int, 1>());
-            else
-                both_halves(std::false_type(), std::integral_constant<int, 2>());
+            });
             load_values<D, kAux>(r, m, g, v);
             cur = nxt;
         }
     }
 
-    // join the wavefronts: lane (m, g) of tile i holds column 16 i + m, dimensions (4 g + x) DL + j
+    const int64_t rows = static_cast<int64_t>(tok.n_tokens) * heads;
+    // the row of column c's results: of its token, of its slot if they are partial
+    const auto row_of = [&](int c, bool& all) {
+        const int slot = at + c / a.ratio, head = h * a.ratio + c % a.ratio;
+        all = kOwn && whole;
+        if (!all) return (kOwn ? a.most[0] + split : split) * rows + static_cast<int64_t>(slot) * heads + head;
+        const int t = px.token(slot, tok.n_tokens);
+        return t < 0 ? int64_t(-1) : static_cast<int64_t>(t) * heads + head;
+    };
+    if constexpr (kAlone) {
+        put_columns<T, D, 1>(a, out, acc, 0, columns, m, g, row_of);
+        return;
+    }
+    // join the wavefronts
+    float(*s_o)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(smem);
+    float(*s_m)[16] = reinterpret_cast<float(*)[16]>(smem + kWaves * 16 * (D + 4));
+    float(*s_l)[16] = s_m + kWaves;
+    const float l0 = sum_groups(acc.l[0]);
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-        const float l = sum_groups(acc.l[i]);
-        const int c = 16 * i + m;
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int j = 0; j < DL; ++j) s_o[wave][c][(4 * g + x) * DL + j] = acc.o[i][j][x];
-        if (g == 0) {
-            s_m[wave][c] = acc.m[i];
-            s_l[wave][c] = l;
-        }
+        for (int j = 0; j < DL; ++j) s_o[wave][m][(4 * g + x) * DL + j] = acc.o[0][j][x];
+    if (g == 0) {
+        s_m[wave][m] = acc.m[0];
+        s_l[wave][m] = l0;
     }
     __syncthreads();
-    for (int i = tid; i < columns * D; i += kThreads) {
-        const int r = i / D, c = i % D;
-        float top = s_m[0][r];
+    // four dimensions of a column a thread
+    for (int i = tid; i < columns * (D / 4); i += kThreads) {
+        const int c = i / (D / 4), dim = i % (D / 4) * 4;
+        float top = s_m[0][c];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][c]);
         const float ref = top == -INFINITY ? 0.f : top;
-        float l = 0.f, sum = 0.f;
+        float l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float f = part_weight(s_m[w][r], ref);
-            l += f * s_l[w][r];
-            sum += f * s_o[w][r][c];
+            const float f = part_weight(s_m[w][c], ref);
+            l += f * s_l[w][c];
+            add_scaled(o, f, *reinterpret_cast<const float4*>(&s_o[w][c][dim]));
         }
-        const int slot = at + r / a.ratio, head = h * a.ratio + r % a.ratio;
-        if (whole) {
-            const int t = px.token(slot, tok.n_tokens);
-            if (t < 0) continue;
-            const int64_t at_row = static_cast<int64_t>(t) * heads + head;
-            out[at_row * D + c] = elem<T>::from_f32(l == 0.f ? 0.f : sum / l);
-            if (a.lse && c == 0) a.lse[at_row] = natural_lse(ref, l);
-        } else {
-            const int64_t to_row = (static_cast<int64_t>(kOwn ? a.most[0] + split : split) * tok.n_tokens + slot) * heads + head;
-            a.part[to_row * D + c] = sum;
-            if (c == 0) {
-                a.part_ml[2 * to_row] = top;
-                a.part_ml[2 * to_row + 1] = l;
-            }
-        }
+        bool all;
+        const int64_t row = row_of(c, all);
+        if (row >= 0) put4<T, D>(a, out, all, row, dim, o, top, l);
     }
 }
 
-template <typename T, int D, int kTiles, int kOwnTiles, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 2) void attend_shared_kernel(PoolView pool, TokensView tok, PrefixView px,
-                                                                       SharedArgs a, const T* __restrict__ q,
-                                                                       int64_t q_stride, T* __restrict__ out) {
+// A wavefront's share of decoding a page that the workgroup uses: words of key codes, of one 16-key tile; and the codes and
+// scales of half the page's values, of which it decodes kPairs dimensions 2 j, 2 j + 1 of the lane's.
+template <int D>
+struct RawPage {
+    static constexpr int kSteps = D / 32, kWords = 4 * kSteps / kWaves, kPairs = 2 * kSteps / kWaves;
+    uint32_t k[kWords], ks, v[2][D / 32], vs[4];
+
+    __device__ __forceinline__ void load(buf_rsrc r, int cg, int m, int g) {
+        using F = PageFormat<D>;
+        const int t = cg * kWords / kSteps, kk = cg * kWords % kSteps, u = cg * kPairs / kSteps;
+        const uint32_t key = F::key_code(16 * t + m, g * (D / 4) + 8 * kk);
+        if constexpr (kWords == 4) {
+            const vec16 x = buf_load16(r, key);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = x.w[i];
+        } else {
+            const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, key, 0, 0));
+            k[0] = x.x;
+            k[1] = x.y;
+        }
+        ks = static_cast<uint32_t>(buf_load_i32(r, F::key_scale(m, g * (D / 4) / 32)));
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            load_codes<D, 0>(r, F::value_code(4 * g, m * F::kLaneDims) + (2 * u + b) * (F::value_code(16, 0) - F::kCodes), v[b]);
+        const vec16 x = buf_load16(r, F::value_scale(4 * g, m * F::kLaneDims / 32));
+#pragma unroll
+        for (int t4 = 0; t4 < 4; ++t4) vs[t4] = x.w[t4];
+    }
+    // Into the page's operands in LDS: [4 tiles][kSteps] of keys, [2 halves][D/16 dimensions] of values, a wavefront's 64
+    // lanes each.
+    template <bool kHalf>
+    __device__ __forceinline__ void store(u32x4* page, int cg, int lane) const {
+        const int t = cg * kWords / kSteps, kk = cg * kWords % kSteps, u = cg * kPairs / kSteps, j0 = cg * kPairs % kSteps;
+        const float scale = scale_of(ks >> (8 * t) & 255u);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+            page[(t * kSteps + kk + i) * 64 + lane] =
+                u32x4{decode2<0>(k[i], scale), decode2<1>(k[i], scale), decode2<2>(k[i], scale), decode2<3>(k[i], scale)};
+        float s[2][4];
+        row_scales(u ? vs[2] : vs[0], u ? vs[3] : vs[1], s);
+        uint32_t c[2][D / 32];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) c[b][i] = v[b][i] >> (8 * j0);
+        u32x4* to = page + (4 * kSteps + (u * kSteps + j0) * 2) * 64 + lane;
+        each(std::make_integer_sequence<int, kPairs>(), [&](auto at) {
+            constexpr int j = decltype(at)::value;
+            u32x4 even, odd;
+            value_pair<D, kHalf, j>(c[0], c[1], s, even, odd);
+            to[2 * j * 64] = even;
+            to[(2 * j + 1) * 64] = odd;
+        });
+    }
+};
+
+// Many columns of one group, kTiles tiles a wavefront, against run `split` of its pages.  The wavefronts decode a page once,
+// a share each, into LDS, while they multiply the page before.
+template <typename T, int D, int kTiles>
+__device__ __forceinline__ void attend_wide(const PoolView& pool, const TokensView& tok, const PrefixView& px,
+                                            const SharedArgs& a, const T* __restrict__ q, int64_t q_stride, float* smem, int h,
+                                            int at, int n_slots, int shared, int split) {
+    using F = PageFormat<D>;
+    constexpr int kSteps = D / 32, kFrags = 8 * kSteps, kTerms = Columns<T, D, kTiles>::kTerms;
+    const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(D));  // log2(e) / sqrt(d)
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, m = lane & 15, g = lane >> 4;
+    u32x4* const pages = reinterpret_cast<u32x4*>(smem);                // [2][kFrags][64]
+    int* const s_of = reinterpret_cast<int*>(smem + 2 * kFrags * 256);  // [wave][3]
+    const int columns = n_slots * a.ratio, c0 = wave * 16 * kTiles, heads = pool.n_kv * a.ratio;
+    const bool idle = c0 >= columns;
+
+    Columns<T, D, kTiles> col;
+    load_columns<T, D, kTiles>(pool, tok, px, a.ratio, q, q_stride, h, at, c0, columns, m, g, col);
+    if (lane == 0) {
+        s_of[3 * wave] = col.s;
+        s_of[3 * wave + 1] = col.last;
+        s_of[3 * wave + 2] = col.first;
+    }
+    __syncthreads();
+    int s = 0, last = -1, first = INT32_MAX;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        s = max(s, s_of[3 * w]);
+        last = max(last, s_of[3 * w + 1]);
+        first = min(first, s_of[3 * w + 2]);
+    }
+    s = __builtin_amdgcn_readfirstlane(s);
+    last = __builtin_amdgcn_readfirstlane(last);
+    first = __builtin_amdgcn_readfirstlane(first);
+    const PageRun run = page_run(split, shared, a.run[0], a.most[0]);
+    const int to = last < 0 ? run.a : min(run.b, last / kPageRows + 1);
+    const bool inside = first < to * kPageRows - 1;  // a token inside these pages
+
+    Acc<D, kTiles> acc;
+    clear(acc);
+    uint32_t poison = 0;
+    for (int e0 = run.a; e0 < to; e0 += 64) {
+        // the next 64 pages, one a lane
+        SeenPage mine{-1, 0};
+        if (e0 + lane < to) mine = seen_page(pool, tok, s, last, e0 + lane);
+        uint64_t left = __builtin_amdgcn_ballot_w64(mine.rows > 0);
+        if (!left) continue;
+        const auto part = [&](int i) {
+            return make_rsrc(pool.page(__builtin_amdgcn_readlane(mine.id, i)) + h * F::kBytes, F::kBytes);
+        };
+        RawPage<D> raw;
+        // the page in `raw`, of lane i, into LDS; whether its values fit f16, whether it holds any that are not numbers
+        // (looked at where a token may not see them)
+        const auto put = [&](int i, int buf, bool& fit, bool& nan) {
+            nan = false;
+            if (__builtin_expect(inside, 0)) {
+                __asm__ volatile("");
+                cut_rows(raw.vs, g, __builtin_amdgcn_readlane(mine.rows, i));
+                uint32_t any = 0;
+#pragma unroll
+                for (int tt = 0; tt < 4; ++tt) {
+                    const uint32_t w = raw.vs[tt], is = nan_bytes(w);
+                    any |= is;
+                    raw.vs[tt] = w ^ is;  // a scale of 1
+                }
+                nan = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+            }
+            fit = sizeof(T) == 4 || values_fit(raw.vs);
+            u32x4* const page = pages + buf * kFrags * 64;
+            if (sizeof(T) == 2 && fit)
+                raw.template store<true>(page, wave, lane);
+            else
+                raw.template store<false>(page, wave, lane);
+        };
+        int cur = static_cast<int>(__builtin_ctzll(left)), buf = 0;
+        left &= left - 1;
+        bool fit, nan;
+        raw.load(part(cur), wave, m, g);
+        put(cur, 0, fit, nan);
+        int nxt = left ? static_cast<int>(__builtin_ctzll(left)) : -1;
+        left &= left - 1;
+        if (nxt >= 0) raw.load(part(nxt), wave, m, g);
+        __syncthreads();
+        // A page; kUsual: one that fits f16 and that every column sees.
+        const auto step = [&](auto usual) {
+            constexpr bool kUsual = decltype(usual)::value;
+            bool fit_next = false, nan_next = false;
+            int after = -1;
+            if (nxt >= 0) {
+                put(nxt, buf ^ 1, fit_next, nan_next);
+                if (left) {
+                    after = static_cast<int>(__builtin_ctzll(left));
+                    left &= left - 1;
+                    raw.load(part(after), wave, m, g);
+                }
+            }
+            if (!idle) {
+                const u32x4* const page = pages + buf * kFrags * 64 + lane;
+                f32x4 sc[kTiles][4];
+                // the next tile's keys are on their way while one is multiplied
+                u32x4 kf[2][kSteps];
+#pragma unroll
+                for (int kk = 0; kk < kSteps; ++kk) kf[0][kk] = page[kk * 64];
+#pragma unroll
+                for (int tt = 0; tt < 4; ++tt) {
+                    if (tt < 3)
+#pragma unroll
+                        for (int kk = 0; kk < kSteps; ++kk) kf[(tt + 1) % 2][kk] = page[((tt + 1) * kSteps + kk) * 64];
+#pragma unroll
+                    for (int i = 0; i < kTiles; ++i) sc[i][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int kk = 0; kk < kSteps; ++kk)
+#pragma unroll
+                        for (int x = 0; x < kTerms; ++x)
+#pragma unroll
+                            for (int i = 0; i < kTiles; ++i) sc[i][tt] = mfma(kf[tt % 2][kk], col.qf[i][x][kk], sc[i][tt]);
+                }
+                if constexpr (!kUsual) {
+                    const int row0 = (e0 + cur) * kPageRows;
+                    int seen[kTiles];
+#pragma unroll
+                    for (int i = 0; i < kTiles; ++i) seen[i] = inside ? col.pos[i] - row0 : kPageRows;
+                    hide_rows<kTiles>(seen, g, sc);
+                    if (nan) {
+                        Values<D> v;
+                        load_values<D, 0>(part(cur), m, g, v);
+                        cut_rows(v.s, g, __builtin_amdgcn_readlane(mine.rows, cur));
+                        poison |= nan_reached<D, kTiles>(v, m, g, seen);
+                    }
+                }
+                raise_reference<D, kTiles>(sc, scale, acc);
+                const auto values = [&](auto half, auto terms) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+                        half_page<D, decltype(half)::value, decltype(terms)::value, kTiles>(u, sc, scale, [&](auto j, u32x4& even, u32x4& odd) {
+                            const u32x4* from = page + (4 * kSteps + (u * kSteps + decltype(j)::value) * 2) * 64;
+                            even = from[0];
+                            odd = from[64];
+                        }, acc);
+                };
+                if constexpr (kUsual)
+                    values(std::bool_constant<sizeof(T) == 2>(), std::integral_constant<int, sizeof(T) == 2 ? 1 : 3>());
+                else
+                    by_terms<T>(fit, values);
+            }
+            __syncthreads();
+            cur = nxt;
+            nxt = after;
+            fit = fit_next;
+            nan = nan_next;
+            buf ^= 1;
+        };
+        // (loops of their own: the rare pages' registers stay out of the others')
+        while (cur >= 0) {
+            while (cur >= 0 && fit && !inside) step(std::true_type());
+            while (cur >= 0 && (!fit || inside)) step(std::false_type());
+        }
+    }
+    set_nan<D, kTiles>(poison, acc);
+    const int64_t rows = static_cast<int64_t>(tok.n_tokens) * heads;
+    put_columns<T, D, kTiles>(a, static_cast<T*>(nullptr), acc, c0, columns, m, g, [&](int c, bool& whole) {
+        whole = false;
+        return split * rows + static_cast<int64_t>(at + c / a.ratio) * heads + h * a.ratio + c % a.ratio;
+    });
+}
+
+// A unit of own pages, sequence by sequence.
+template <typename T, int D, bool kAlone>
+__device__ __forceinline__ void attend_own(const PoolView& pool, const TokensView& tok, const PrefixView& px,
+                                           const SharedArgs& a, const T* __restrict__ q, int64_t q_stride, T* __restrict__ out,
+                                           float* smem, int h, int unit, int split) {
+    const int lane = threadIdx.x & 63;
+    const int from = unit * a.slots[1], n = min(a.slots[1], tok.n_tokens - from);
+    // a lane a slot: where a run of slots of one sequence and group begins
+    int group = -1, seq = -1;
+    if (lane < n) {
+        const int t = px.token(from + lane, tok.n_tokens);
+        seq = t < 0 ? -1 : tok.seq[t];
+        group = group_of(px, tok.n_tokens, from + lane);
+        if (t < 0) group = -2;  // no token: a run of its own
+    }
+    const int seq_before = __shfl_up(seq, 1), group_before = __shfl_up(group, 1);
+    const bool begins = lane == 0 || group == -2 || seq != seq_before || group != group_before;
+    uint64_t left = __builtin_amdgcn_ballot_w64(lane < n && begins);
+    while (left) {
+        const int i = static_cast<int>(__builtin_ctzll(left));
+        left &= left - 1;
+        const int end = left ? static_cast<int>(__builtin_ctzll(left)) : n, gi = __builtin_amdgcn_readlane(group, i);
+        attend_slots<T, D, true, kAlone>(pool, tok, px, a, q, q_stride, out, smem, h, from + i, end - i,
+                                         gi < 0 ? 0 : px.shared(gi, tok.max_pages), split);
+        if constexpr (!kAlone) __syncthreads();  // LDS is the next sequence's
+    }
+}
+
+// The groups' units first, then the tokens' own pages; a unit's runs stand in the outer order.  kTiles 0: groups of few columns.
+template <typename T, int D, int kTiles>
+__global__ __launch_bounds__(kThreads, 2) void attend_shared_kernel(PoolView pool, TokensView tok, PrefixView px, SharedArgs a,
+                                                                    const T* __restrict__ q, int64_t q_stride,
+                                                                    T* __restrict__ out) {
     extern __shared__ __align__(16) float smem[];
-    // the groups' runs first, then the tokens' own; a unit's runs in the outer order
-    uint32_t block = linear_block<64 * kWaves>();
-    const uint32_t n_group = static_cast<uint32_t>(a.units[0]) * pool.n_kv * a.most[0];
-    const bool own = block >= n_group;
-    if (own) block -= n_group;
-    const uint32_t row = static_cast<uint32_t>(a.units[own]) * pool.n_kv;
-    if (block >= row * static_cast<uint32_t>(a.most[own])) return;
-    const int split = static_cast<int>(block / row);
-    const TokenHead where = token_head(block % row, pool.n_kv);
-    if (!own) {
+    uint32_t block = linear_block<kThreads>();
+    const uint32_t of_group = static_cast<uint32_t>(a.units[0]) * pool.n_kv, n_group = of_group * a.most[0];
+    if (block < n_group) {
+        const int split = static_cast<int>(block / of_group);
+        const TokenHead where = token_head(block % of_group, pool.n_kv);
         const GroupUnit u = group_unit(px, tok.n_tokens, a.slots[0], where.t);
         if (u.g < 0) return;
         const int shared = px.shared(u.g, tok.max_pages);
         if (split >= runs_of(shared, a.run[0], a.most[0])) return;
-        attend_slots<T, D, kTiles, kWaves, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, u.a, u.b - u.a, shared,
-                                                  split);
+        if constexpr (kTiles == 0)
+            attend_slots<T, D, false, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, u.a, u.b - u.a, shared, split);
+        else
+            attend_wide<T, D, kTiles>(pool, tok, px, a, q, q_stride, smem, where.h, u.a, u.b - u.a, shared, split);
         return;
     }
-    // a unit of own pages sequence by sequence
-    const int end = min((where.t + 1) * a.slots[1], tok.n_tokens);
-    for (int at = where.t * a.slots[1], next; at < end; at = next) {
-        const int group = group_of(px, tok.n_tokens, at);
-        const int first = px.token(at, tok.n_tokens), seq = first < 0 ? -1 : tok.seq[first];
-        // the slots behind it of the same sequence and group
-        for (next = at + 1; next < end; ++next) {
-            const int t = px.token(next, tok.n_tokens);
-            if (t < 0 || first < 0 || tok.seq[t] != seq || group_of(px, tok.n_tokens, next) != group) break;
-        }
-        attend_slots<T, D, kOwnTiles, kWaves, true>(pool, tok, px, a, q, q_stride, out, smem, where.h, at, next - at,
-                                                    group < 0 ? 0 : px.shared(group, tok.max_pages), split);
-        __syncthreads();  // LDS is the next sequence's
+    block -= n_group;
+    const uint32_t of_own = static_cast<uint32_t>(a.units[1]) * pool.n_kv;
+    if (a.alone) {
+        // (one run a unit)
+        const uint32_t item = block * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (item >= of_own) return;
+        const TokenHead where = token_head(item, pool.n_kv);
+        attend_own<T, D, true>(pool, tok, px, a, q, q_stride, out, smem, where.h, where.t, 0);
+    } else {
+        const int split = static_cast<int>(block / of_own);
+        if (split >= a.most[1]) return;
+        const TokenHead where = token_head(block % of_own, pool.n_kv);
+        attend_own<T, D, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, where.t, split);
     }
 }
 
-// Joins the partial results of a slot's query head, in a fixed order: a workgroup a head, its threads D/4 columns of four
-// dimensions by the groups of parts they add up.
-template <typename T, int D>
+// Joins the partial results of a slot's query head, in a fixed order.  Its D / 4 columns of four dimensions are a thread
+// each; kTeams of them take parts in turns.
+template <typename T, int D, int kTeams>
 __global__ __launch_bounds__(256) void join_shared_kernel(int n_tokens, int heads, PrefixView px, SharedArgs a,
                                                           T* __restrict__ out) {
-    constexpr int kCols = D / 4, kGroups = 256 / kCols;
-    __shared__ float4 s_o[kGroups][kCols];
-    __shared__ float s_l[kGroups], s_m[kGroups];
-    const int64_t row = linear_block<256>(), rows = static_cast<int64_t>(n_tokens) * heads;
-    if (row >= rows) return;
-    const int slot = static_cast<int>(row / heads), head = static_cast<int>(row % heads);
-    const int t = px.token(slot, n_tokens);
-    const int of_group = a.counts[2 * slot], of_own = a.counts[2 * slot + 1], parts = of_group + of_own;
-    if (t < 0 || (of_group == 0 && of_own <= 1)) return;
-    const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
+    constexpr int kCols = D / 4, kRows = 256 / kCols / kTeams;
+    __shared__ float4 s_o[kTeams][kRows][kCols];
+    __shared__ float s_l[kTeams][kRows], s_m[kTeams][kRows];
+    const int col = threadIdx.x % kCols, sub = threadIdx.x / kCols % kRows, team = threadIdx.x / kCols / kRows;
+    const int64_t row = static_cast<int64_t>(linear_block<256>()) * kRows + sub, rows = static_cast<int64_t>(n_tokens) * heads;
+    const bool real = row < rows;
+    const int slot = real ? static_cast<int>(row / heads) : 0, head = static_cast<int>(row % heads);
+    const int t = real ? px.token(slot, n_tokens) : -1;
+    const int of_group = a.counts[2 * slot], of_own = a.counts[2 * slot + 1];
+    // (the result of a single run of own pages is there)
+    const int parts = t < 0 || (of_group == 0 && of_own <= 1) ? 0 : of_group + of_own;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int w0 = grp; w0 < parts; w0 += 4 * kGroups) {
+    for (int w0 = team; w0 < parts; w0 += 4 * kTeams) {
         float2 ml[4];
         float4 x[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-            const int w = min(w0 + y * kGroups, parts - 1);
+            const int w = min(w0 + y * kTeams, parts - 1);
             const int64_t at = (w < of_group ? w : a.most[0] + w - of_group) * rows + row;
             ml[y] = reinterpret_cast<const float2*>(a.part_ml)[at];
             x[y] = reinterpret_cast<const float4*>(a.part)[at * kCols + col];
         }
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-            if (w0 + y * kGroups >= parts) break;
+            if (w0 + y * kTeams >= parts) break;
             const float top = fmaxf(m, ml[y].x), ref = top == -INFINITY ? 0.f : top;
             const float f = part_weight(m, ref), e = part_weight(ml[y].x, ref);
             m = top;
             l = l * f + ml[y].y * e;
-            o.x = o.x * f + x[y].x * e;
-            o.y = o.y * f + x[y].y * e;
-            o.z = o.z * f + x[y].z * e;
-            o.w = o.w * f + x[y].w * e;
+            o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+            add_scaled(o, e, x[y]);
         }
     }
-    s_o[grp][col] = o;
-    if (col == 0) {
-        s_m[grp] = m;
-        s_l[grp] = l;
-    }
-    __syncthreads();
-    if (threadIdx.x >= D) return;
-    float top = s_m[0];
+    if constexpr (kTeams > 1) {
+        s_o[team][sub][col] = o;
+        if (col == 0) {
+            s_m[team][sub] = m;
+            s_l[team][sub] = l;
+        }
+        __syncthreads();
+        if (team > 0) return;
+        m = s_m[0][sub];
 #pragma unroll
-    for (int w = 1; w < kGroups; ++w) top = fmaxf(top, s_m[w]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    l = 0.f;
+        for (int w = 1; w < kTeams; ++w) m = fmaxf(m, s_m[w][sub]);
+        const float ref = m == -INFINITY ? 0.f : m;
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+        l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kGroups; ++w) {
-        const float f = part_weight(s_m[w], ref);
-        l += f * s_l[w];
-        sum += f * reinterpret_cast<const float*>(s_o[w])[threadIdx.x];
+        for (int w = 0; w < kTeams; ++w) {
+            const float f = part_weight(s_m[w][sub], ref);
+            l += f * s_l[w][sub];
+            add_scaled(o, f, s_o[w][sub][col]);
+        }
     }
-    const int64_t to = static_cast<int64_t>(t) * heads + head;
-    out[to * D + threadIdx.x] = elem<T>::from_f32(l == 0.f ? 0.f : sum / l);
-    if (a.lse && threadIdx.x == 0) a.lse[to] = natural_lse(ref, l);
+    if (parts == 0) return;
+    put4<T, D>(a, out, true, static_cast<int64_t>(t) * heads + head, 4 * col, o, m, l);
 }
+
+// How a call is cut: columns of a tile row, slots of a unit, pages of a run and runs of a unit at most, units; [0] the groups'
+// pages, [1] the tokens' own.
+struct Cut {
+    int tiles;  // of a wavefront of a group's unit; 0: the unit is one tile, for few columns
+    int slots[2], run[2], most[2], units[2];
+    bool alone;
+    int64_t part, part_ml, bytes;  // the workspace, in bytes from its start
+};
 
 int64_t pad16(int64_t n) { return (n + 15) / 16 * 16; }
 
-// Tiles of a group's unit: two, but for fp32 at 128 dimensions (registers).
-template <typename T, int D>
-constexpr int kTilesOf = sizeof(T) == 4 && D == 128 ? 1 : 2;
-
 Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int n_groups, int shared_hint, int own_hint,
              int64_t ws_bytes) {
-    const int ratio = plan.p.n_q_heads / plan.p.n_kv_heads;
-    const int tiles = plan.p.dtype == HGA_F32 && plan.p.head_dim == 128 ? 1 : 2;
+    const int ratio = plan.p.n_q_heads / plan.p.n_kv_heads, kv = plan.p.n_kv_heads;
     const int64_t rows = static_cast<int64_t>(n_tokens) * plan.p.n_q_heads;
-    Cut c{};
-    const int most_slots = 16 * tiles / ratio;
-    const int per_seq = static_cast<int>((static_cast<int64_t>(n_tokens) + n_seqs - 1) / std::max(n_seqs, 1));
-    c.slots[0] = most_slots;
-    c.slots[1] = std::clamp(per_seq, 1, most_slots);
-    c.units[0] = n_groups ? static_cast<int>(std::min<int64_t>(n_tokens, n_tokens / most_slots + static_cast<int64_t>(n_groups))) : 0;
-    c.units[1] = (n_tokens + c.slots[1] - 1) / c.slots[1];
     const int64_t pages[2] = {std::clamp(shared_hint, 1, std::max(max_pages, 1)), std::clamp(own_hint, 1, std::max(max_pages, 1))};
-    const int64_t want = 4 * static_cast<int64_t>(plan.n_cu);
+    const int64_t cus = plan.n_cu;
+    const auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+    Cut c{};
+    // by the columns that a group has on average
+    const int64_t columns = static_cast<int64_t>(n_tokens) * ratio / std::max(n_groups, 1);
+    c.tiles = columns <= 16 ? 0 : columns <= 64 || (plan.p.dtype == HGA_F32 && plan.p.head_dim == 128) ? 1 : 2;
+    c.slots[0] = 16 * (c.tiles ? c.tiles * kWaves : 1) / ratio;
+    const int per_seq = static_cast<int>(up(n_tokens, std::max(n_seqs, 1)));
+    c.slots[1] = std::clamp(per_seq, 1, 16 / ratio);
+    // a group's last unit may be a small one
+    c.units[0] = n_groups ? static_cast<int>(std::min<int64_t>(n_tokens, n_tokens / c.slots[0] + static_cast<int64_t>(n_groups))) : 0;
+    c.units[1] = static_cast<int>(up(n_tokens, c.slots[1]));
     for (int i = 0; i < 2; ++i) {
-        const int64_t units = static_cast<int64_t>(c.units[i]) * plan.p.n_kv_heads;
+        const int64_t units = kv * (i ? c.units[1] : std::max(up(n_tokens, c.slots[0]), static_cast<int64_t>(n_groups)));
         c.run[i] = static_cast<int>(pages[i]);
         c.most[i] = 1;
-        if (units == 0 || units >= want) continue;
-        const int64_t run = std::max<int64_t>(16, (units * pages[i] + want - 1) / want);
-        c.most[i] = static_cast<int>((pages[i] + run - 1) / run);
-        c.run[i] = static_cast<int>((pages[i] + c.most[i] - 1) / c.most[i]);
+        if (c.units[i] == 0 || units >= 2 * cus) continue;
+        const int64_t run = std::max<int64_t>(i ? 16 : 8, up(units * pages[i], 2 * cus));
+        c.most[i] = static_cast<int>(up(pages[i], run));
+        c.run[i] = static_cast<int>(up(pages[i], c.most[i]));
     }
+    // Own pages by a wavefront or a workgroup: what a round of workgroups takes, in pages, about five of them for what comes
+    // before the first.
+    const int64_t own = static_cast<int64_t>(c.units[1]) * kv;
+    c.alone = c.most[1] == 1 && up(own, 2 * kWaves * cus) * (5 + pages[1]) <= up(own, 2 * cus) * (5 + up(pages[1], kWaves));
     const int64_t counts = pad16(static_cast<int64_t>(n_tokens) * 8);
     // fewer runs where the workspace holds no more
     const int64_t run_bytes = rows * (plan.p.head_dim + 2) * 4;
     const int64_t room = ws_bytes < counts ? 0 : (ws_bytes - counts) / run_bytes;
     while (c.most[0] + c.most[1] > room && (c.most[0] > 1 || c.most[1] > 1)) {
         const int i = c.most[0] >= c.most[1] ? 0 : 1;
-        c.run[i] = static_cast<int>((pages[i] + --c.most[i] - 1) / std::max(c.most[i], 1));
+        c.run[i] = static_cast<int>(up(pages[i], --c.most[i]));
     }
     c.part = counts;
     c.part_ml = c.part + (c.most[0] + c.most[1]) * rows * plan.p.head_dim * 4;
@@ -530,28 +875,37 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
     return c;
 }
 
-template <typename T, int D, int kOwnTiles>
+template <typename T, int D, int kTiles>
 hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const PrefixView& px, const SharedArgs& a,
                const void* q, int64_t q_stride, void* out, hipStream_t stream) {
-    constexpr int kTiles = kTilesOf<T, D>, kWaves = 4, kThreads = 64 * kWaves;
-    constexpr size_t lds = sizeof(float) * kWaves * 16 * kTiles * (D + 4 + 2);
-    if (lds > 65536) {
+    constexpr size_t kJoin = sizeof(float) * kWaves * 16 * (D + 4 + 2);
+    constexpr size_t kPages = kTiles ? 2 * (D / 4) * 1024 + 3 * kWaves * 4 : 0;
+    constexpr size_t lds = std::max(kJoin, kPages);
+    const auto kernel = attend_shared_kernel<T, D, kTiles>;
+    hipError_t e;
+    if constexpr (lds > 65536) {
         static std::atomic<uint64_t> done{0};
-        const hipError_t e = once_per_device(done, plan.device, [] {
-            return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_shared_kernel<T, D, kTiles, kOwnTiles, kWaves>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+        e = once_per_device(done, plan.device, [=] {
+            return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(lds));
         });
         if (e != hipSuccess) return e;
     }
-    const int64_t n = static_cast<int64_t>(pool.n_kv) *
-                      (static_cast<int64_t>(a.units[0]) * a.most[0] + static_cast<int64_t>(a.units[1]) * a.most[1]);
-    attend_shared_kernel<T, D, kTiles, kOwnTiles, kWaves><<<grid_of(n, kThreads), kThreads, lds, stream>>>(
-        pool, tok, px, a, static_cast<const T*>(q), q_stride, static_cast<T*>(out));
-    const hipError_t e = hipGetLastError();
+    const int64_t own = static_cast<int64_t>(pool.n_kv) * a.units[1];
+    const int64_t n = static_cast<int64_t>(pool.n_kv) * a.units[0] * a.most[0] +
+                      (a.alone ? (own + kWaves - 1) / kWaves : own * a.most[1]);
+    kernel<<<grid_of(n, kThreads), kThreads, lds, stream>>>(pool, tok, px, a, static_cast<const T*>(q), q_stride,
+                                                            static_cast<T*>(out));
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int heads = pool.n_kv * a.ratio;
-    join_shared_kernel<T, D><<<grid_of(static_cast<int64_t>(tok.n_tokens) * heads, 256), 256, 0, stream>>>(
-        tok.n_tokens, heads, px, a, static_cast<T*>(out));
+    const int64_t rows = static_cast<int64_t>(tok.n_tokens) * heads;
+    constexpr int kRows = 256 / (D / 4);
+    if (a.most[0] + a.most[1] <= 4)
+        join_shared_kernel<T, D, 1><<<grid_of((rows + kRows - 1) / kRows, 256), 256, 0, stream>>>(tok.n_tokens, heads, px, a,
+                                                                                                  static_cast<T*>(out));
+    else
+        join_shared_kernel<T, D, kRows><<<grid_of(rows, 256), 256, 0, stream>>>(tok.n_tokens, heads, px, a, static_cast<T*>(out));
     return hipGetLastError();
 }
 
@@ -575,6 +929,7 @@ hipError_t launch_attend_shared(const hga_plan& plan, const PoolView& pool, cons
         a.most[i] = c.most[i];
         a.units[i] = c.units[i];
     }
+    a.alone = c.alone;
     a.lse = lse;
     char* w = static_cast<char*>(ws);
     a.counts = reinterpret_cast<int32_t*>(w);
@@ -582,9 +937,8 @@ hipError_t launch_attend_shared(const hga_plan& plan, const PoolView& pool, cons
     a.part_ml = reinterpret_cast<float*>(w + c.part_ml);
     const auto go = [&](auto zero, auto dim) {
         using T = decltype(zero);
-        constexpr int D = decltype(dim)::value;
-        // one tile where a sequence's slots fill no more
-        const auto f = c.slots[1] * a.ratio > 16 ? run<T, D, kTilesOf<T, D>> : run<T, D, 1>;
+        constexpr int D = decltype(dim)::value, kMost = sizeof(T) == 4 && D == 128 ? 1 : 2;
+        const auto f = c.tiles == 0 ? run<T, D, 0> : c.tiles == 1 ? run<T, D, 1> : run<T, D, kMost>;
         return f(plan, pool, tok, px, a, q, q_stride, out, stream);
     };
     const bool f32 = plan.p.dtype == HGA_F32;
