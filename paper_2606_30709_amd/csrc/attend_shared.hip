@@ -38,29 +38,46 @@ __device__ __forceinline__ uint32_t decode2h(uint32_t codes, float scale) {
 }
 
 // Whether every scale of a page's values has an exponent byte of 109 .. 140.
-__device__ __forceinline__ bool values_fit(const uint32_t (&s)[4]) {
-    uint32_t any = 0, all = ~0u;
+struct ScaleRange {
+    uint32_t any = 0, all = ~0u;  // of the bytes + 19: 128 .. 159 (one that carries into the next is out of range itself)
+
+    __device__ __forceinline__ void add(const uint32_t (&s)[4]) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const uint32_t w = s[t] + 0x13131313u;  // 128 .. 159; a byte that carries into the next is out of range itself
-        any |= w;
-        all &= w;
+        for (int t = 0; t < 4; ++t) {
+            const uint32_t w = s[t] + 0x13131313u;
+            any |= w;
+            all &= w;
+        }
     }
-    return !__builtin_amdgcn_ballot_w64((any & 0x60606060u) != 0 || (~all & 0x80808080u) != 0);
+    __device__ __forceinline__ bool fits() const {
+        return !__builtin_amdgcn_ballot_w64((any & 0x60606060u) != 0 || (~all & 0x80808080u) != 0);
+    }
+};
+__device__ __forceinline__ bool values_fit(const uint32_t (&s)[4]) {
+    ScaleRange r;
+    r.add(s);
+    return r.fits();
 }
 
-// The running reference of every column, raised where a lane's scores exceed it by more than the slack.
-template <int D, int kTiles>
-__device__ __forceinline__ void raise_reference(const f32x4 (&sc)[kTiles][4], float scale, Acc<D, kTiles>& acc) {
+// The largest of a lane's scores.
+template <int kTiles>
+__device__ __forceinline__ void largest(const f32x4 (&sc)[kTiles][4], float (&top)[kTiles]) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-        float top = sc[i][0][0];
+        top[i] = sc[i][0][0];
 #pragma unroll
         for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) top = fmaxf(top, sc[i][tt][x]);
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(top * scale > acc.m[i] + kTop) != 0, 0)) {
-            top = max_groups(top) * scale;
+            for (int x = 0; x < 4; ++x) top[i] = fmaxf(top[i], sc[i][tt][x]);
+    }
+}
+// The running reference of every column, raised where a lane's scores exceed it by more than the slack.
+template <int D, int kTiles>
+__device__ __forceinline__ void raise_reference(const float (&tops)[kTiles], float scale, Acc<D, kTiles>& acc) {
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(tops[i] * scale > acc.m[i] + kTop) != 0, 0)) {
+            const float top = max_groups(tops[i]) * scale;
             const bool grow = top > acc.m[i] + kTop;
             const float to = top - kLead;
             const float alpha = grow ? __builtin_amdgcn_exp2f(acc.m[i] - to) : 1.f;
@@ -69,7 +86,12 @@ __device__ __forceinline__ void raise_reference(const f32x4 (&sc)[kTiles][4], fl
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) acc.o[i][j] *= alpha;
         }
-    }
+}
+template <int D, int kTiles>
+__device__ __forceinline__ void raise_reference(const f32x4 (&sc)[kTiles][4], float scale, Acc<D, kTiles>& acc) {
+    float top[kTiles];
+    largest<kTiles>(sc, top);
+    raise_reference<D, kTiles>(top, scale, acc);
 }
 
 template <int... kAt, typename F>
@@ -470,17 +492,17 @@ __device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensV
     }
 }
 
-// A wavefront's share of decoding a page that the workgroup uses: words of key codes, of one 16-key tile; and the codes and
-// scales of half the page's values, of which it decodes kPairs dimensions 2 j, 2 j + 1 of the lane's.
+// A wavefront's share of decoding a page that the workgroup uses: words of key codes, of one 16-key tile; and the codes of
+// half the page's values, of which it decodes kPairs dimensions 2 j, 2 j + 1 of the lane's.  In LDS a page is operands of a
+// wavefront's 64 lanes: [4 tiles][kSteps] of keys, then [2 halves][D/16 dimensions] of values.
 template <int D>
-struct RawPage {
-    static constexpr int kSteps = D / 32, kWords = 4 * kSteps / kWaves, kPairs = 2 * kSteps / kWaves;
-    uint32_t k[kWords], ks, v[2][D / 32], vs[4];
+struct RawKeys {
+    static constexpr int kSteps = D / 32, kWords = 4 * kSteps / kWaves;
+    uint32_t k[kWords], s;
 
-    __device__ __forceinline__ void load(buf_rsrc r, int cg, int m, int g) {
+    __device__ __forceinline__ void load(buf_rsrc r, int wave, int m, int g) {
         using F = PageFormat<D>;
-        const int t = cg * kWords / kSteps, kk = cg * kWords % kSteps, u = cg * kPairs / kSteps;
-        const uint32_t key = F::key_code(16 * t + m, g * (D / 4) + 8 * kk);
+        const uint32_t key = F::key_code(16 * wave + m, g * (D / 4));
         if constexpr (kWords == 4) {
             const vec16 x = buf_load16(r, key);
 #pragma unroll
@@ -490,24 +512,35 @@ struct RawPage {
             k[0] = x.x;
             k[1] = x.y;
         }
-        ks = static_cast<uint32_t>(buf_load_i32(r, F::key_scale(m, g * (D / 4) / 32)));
+        s = static_cast<uint32_t>(buf_load_i32(r, F::key_scale(m, g * (D / 4) / 32)));
+    }
+    // word i
+    __device__ __forceinline__ void store(u32x4* page, int wave, int lane, int i) const {
+        const float scale = scale_of(s >> (8 * wave) & 255u);
+        page[(wave * kSteps + i) * 64 + lane] =
+            u32x4{decode2<0>(k[i], scale), decode2<1>(k[i], scale), decode2<2>(k[i], scale), decode2<3>(k[i], scale)};
+    }
+    __device__ __forceinline__ void store(u32x4* page, int wave, int lane) const {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) store(page, wave, lane, i);
+    }
+};
+template <int D>
+struct RawValues {
+    static constexpr int kSteps = D / 32, kPairs = 2 * kSteps / kWaves;
+    uint32_t v[2][D / 32];
+
+    __device__ __forceinline__ void load(buf_rsrc r, int wave, int m, int g) {
+        using F = PageFormat<D>;
+        const int u = wave * kPairs / kSteps;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
             load_codes<D, 0>(r, F::value_code(4 * g, m * F::kLaneDims) + (2 * u + b) * (F::value_code(16, 0) - F::kCodes), v[b]);
-        const vec16 x = buf_load16(r, F::value_scale(4 * g, m * F::kLaneDims / 32));
-#pragma unroll
-        for (int t4 = 0; t4 < 4; ++t4) vs[t4] = x.w[t4];
     }
-    // Into the page's operands in LDS: [4 tiles][kSteps] of keys, [2 halves][D/16 dimensions] of values, a wavefront's 64
-    // lanes each.
-    template <bool kHalf>
-    __device__ __forceinline__ void store(u32x4* page, int cg, int lane) const {
-        const int t = cg * kWords / kSteps, kk = cg * kWords % kSteps, u = cg * kPairs / kSteps, j0 = cg * kPairs % kSteps;
-        const float scale = scale_of(ks >> (8 * t) & 255u);
-#pragma unroll
-        for (int i = 0; i < kWords; ++i)
-            page[(t * kSteps + kk + i) * 64 + lane] =
-                u32x4{decode2<0>(k[i], scale), decode2<1>(k[i], scale), decode2<2>(k[i], scale), decode2<3>(k[i], scale)};
+    // pair kAt
+    template <bool kHalf, int kAt>
+    __device__ __forceinline__ void store(const uint32_t (&vs)[4], u32x4* page, int wave, int lane) const {
+        const int u = wave * kPairs / kSteps, j0 = wave * kPairs % kSteps;
         float s[2][4];
         row_scales(u ? vs[2] : vs[0], u ? vs[3] : vs[1], s);
         uint32_t c[2][D / 32];
@@ -515,180 +548,230 @@ struct RawPage {
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) c[b][i] = v[b][i] >> (8 * j0);
-        u32x4* to = page + (4 * kSteps + (u * kSteps + j0) * 2) * 64 + lane;
-        each(std::make_integer_sequence<int, kPairs>(), [&](auto at) {
-            constexpr int j = decltype(at)::value;
-            u32x4 even, odd;
-            value_pair<D, kHalf, j>(c[0], c[1], s, even, odd);
-            to[2 * j * 64] = even;
-            to[(2 * j + 1) * 64] = odd;
-        });
+        u32x4 even, odd;
+        value_pair<D, kHalf, kAt>(c[0], c[1], s, even, odd);
+        u32x4* to = page + (4 * kSteps + (u * kSteps + j0 + kAt) * 2) * 64 + lane;
+        to[0] = even;
+        to[64] = odd;
+    }
+    template <bool kHalf>
+    __device__ __forceinline__ void store(const uint32_t (&vs)[4], u32x4* page, int wave, int lane) const {
+        each(std::make_integer_sequence<int, kPairs>(),
+             [&](auto at) { store<kHalf, decltype(at)::value>(vs, page, wave, lane); });
     }
 };
+template <int D>
+__device__ __forceinline__ void load_value_scales(buf_rsrc r, int m, int g, uint32_t (&s)[4]) {
+    const vec16 x = buf_load16(r, PageFormat<D>::value_scale(4 * g, m * PageFormat<D>::kLaneDims / 32));
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = x.w[t];
+}
 
 // Many columns of one group, kTiles tiles a wavefront, against run `split` of its pages.  The wavefronts decode a page once,
-// a share each, into LDS, while they multiply the page before.
+// a share each, into LDS.  A page's weights are formed beside the products of the next one's keys, and its values are
+// multiplied beside the decoding of further pages, so that neither unit of a SIMD waits for the other.
+// Only for columns that see all of the run, and for a bf16 call values that fit f16; false: they do not, nothing is stored.
 template <typename T, int D, int kTiles>
-__device__ __forceinline__ void attend_wide(const PoolView& pool, const TokensView& tok, const PrefixView& px,
+__device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensView& tok, const PrefixView& px,
                                             const SharedArgs& a, const T* __restrict__ q, int64_t q_stride, float* smem, int h,
-                                            int at, int n_slots, int shared, int split) {
+                                            int at_slot, int n_slots, int shared, int split) {
     using F = PageFormat<D>;
-    constexpr int kSteps = D / 32, kFrags = 8 * kSteps, kTerms = Columns<T, D, kTiles>::kTerms;
+    constexpr int kSteps = D / 32, kFrags = 8 * kSteps, kTerms = Columns<T, D, kTiles>::kTerms, kParts = sizeof(T) == 4 ? 3 : 1;
+    constexpr bool kHalf = sizeof(T) == 2;
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(D));  // log2(e) / sqrt(d)
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, m = lane & 15, g = lane >> 4;
     u32x4* const pages = reinterpret_cast<u32x4*>(smem);                // [2][kFrags][64]
-    int* const s_of = reinterpret_cast<int*>(smem + 2 * kFrags * 256);  // [wave][3]
+    int* const s_of = reinterpret_cast<int*>(smem + 2 * kFrags * 256);  // [wave][2]
     const int columns = n_slots * a.ratio, c0 = wave * 16 * kTiles, heads = pool.n_kv * a.ratio;
-    const bool idle = c0 >= columns;
 
     Columns<T, D, kTiles> col;
-    load_columns<T, D, kTiles>(pool, tok, px, a.ratio, q, q_stride, h, at, c0, columns, m, g, col);
+    load_columns<T, D, kTiles>(pool, tok, px, a.ratio, q, q_stride, h, at_slot, c0, columns, m, g, col);
+    int s = 0, first = INT32_MAX;  // of the tokens that are some
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) first = min(first, col.pos[i] < 0 ? INT32_MAX : col.pos[i]);
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) first = min(first, __shfl_xor(first, x));
     if (lane == 0) {
-        s_of[3 * wave] = col.s;
-        s_of[3 * wave + 1] = col.last;
-        s_of[3 * wave + 2] = col.first;
+        s_of[2 * wave] = col.s;
+        s_of[2 * wave + 1] = first;
     }
     __syncthreads();
-    int s = 0, last = -1, first = INT32_MAX;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        s = max(s, s_of[3 * w]);
-        last = max(last, s_of[3 * w + 1]);
-        first = min(first, s_of[3 * w + 2]);
+        s = max(s, s_of[2 * w]);
+        first = min(first, s_of[2 * w + 1]);
     }
     s = __builtin_amdgcn_readfirstlane(s);
-    last = __builtin_amdgcn_readfirstlane(last);
     first = __builtin_amdgcn_readfirstlane(first);
     const PageRun run = page_run(split, shared, a.run[0], a.most[0]);
-    const int to = last < 0 ? run.a : min(run.b, last / kPageRows + 1);
-    const bool inside = first < to * kPageRows - 1;  // a token inside these pages
+    if (first < run.b * kPageRows - 1) return false;
 
     Acc<D, kTiles> acc;
     clear(acc);
-    uint32_t poison = 0;
-    for (int e0 = run.a; e0 < to; e0 += 64) {
+    ScaleRange range;
+    for (int e0 = run.a; e0 < run.b; e0 += 64) {
         // the next 64 pages, one a lane
-        SeenPage mine{-1, 0};
-        if (e0 + lane < to) mine = seen_page(pool, tok, s, last, e0 + lane);
-        uint64_t left = __builtin_amdgcn_ballot_w64(mine.rows > 0);
+        int id = -1;
+        if (e0 + lane < run.b) id = tok.page_id(s, e0 + lane);
+        uint64_t left = __builtin_amdgcn_ballot_w64(pool.has(id));
         if (!left) continue;
+        // lane i's page; i -1: an empty one, whose loads return zeros
         const auto part = [&](int i) {
-            return make_rsrc(pool.page(__builtin_amdgcn_readlane(mine.id, i)) + h * F::kBytes, F::kBytes);
+            return make_rsrc(pool.page(__builtin_amdgcn_readlane(id, max(i, 0))) + h * F::kBytes, i >= 0 ? F::kBytes : 0);
         };
-        RawPage<D> raw;
-        // the page in `raw`, of lane i, into LDS; whether its values fit f16, whether it holds any that are not numbers
-        // (looked at where a token may not see them)
-        const auto put = [&](int i, int buf, bool& fit, bool& nan) {
-            nan = false;
-            if (__builtin_expect(inside, 0)) {
-                __asm__ volatile("");
-                cut_rows(raw.vs, g, __builtin_amdgcn_readlane(mine.rows, i));
-                uint32_t any = 0;
-#pragma unroll
-                for (int tt = 0; tt < 4; ++tt) {
-                    const uint32_t w = raw.vs[tt], is = nan_bytes(w);
-                    any |= is;
-                    raw.vs[tt] = w ^ is;  // a scale of 1
-                }
-                nan = __builtin_amdgcn_ballot_w64(any != 0) != 0;
-            }
-            fit = sizeof(T) == 4 || values_fit(raw.vs);
-            u32x4* const page = pages + buf * kFrags * 64;
-            if (sizeof(T) == 2 && fit)
-                raw.template store<true>(page, wave, lane);
-            else
-                raw.template store<false>(page, wave, lane);
+        const auto pop = [&] {
+            const int i = left ? static_cast<int>(__builtin_ctzll(left)) : -1;
+            left &= left - 1;
+            return i;
         };
-        int cur = static_cast<int>(__builtin_ctzll(left)), buf = 0;
-        left &= left - 1;
-        bool fit, nan;
-        raw.load(part(cur), wave, m, g);
-        put(cur, 0, fit, nan);
-        int nxt = left ? static_cast<int>(__builtin_ctzll(left)) : -1;
-        left &= left - 1;
-        if (nxt >= 0) raw.load(part(nxt), wave, m, g);
+        // A page is multiplied, next the keys of n1 (in LDS), whose values are decoded meanwhile with the keys of n2; the
+        // buffers of a page are those of its number's last bit.
+        int n1, n2, bit = 0;
+        RawKeys<D> rk;
+        RawValues<D> rv;
+        uint32_t vs[4], vs_after[4];
+        {
+            const buf_rsrc r = part(pop());
+            n1 = pop();
+            n2 = pop();
+            RawKeys<D> rk1;
+            rk.load(r, wave, m, g);
+            rv.load(r, wave, m, g);
+            load_value_scales<D>(r, m, g, vs);
+            rk1.load(part(n1), wave, m, g);
+            rk.store(pages, wave, lane);
+            range.add(vs);
+            rv.template store<kHalf>(vs, pages, wave, lane);
+            rk1.store(pages + kFrags * 64, wave, lane);
+        }
+        rk.load(part(n2), wave, m, g);
+        rv.load(part(n1), wave, m, g);
+        load_value_scales<D>(part(n1), m, g, vs);
+        load_value_scales<D>(part(n2), m, g, vs_after);
         __syncthreads();
-        // A page; kUsual: one that fits f16 and that every column sees.
-        const auto step = [&](auto usual) {
-            constexpr bool kUsual = decltype(usual)::value;
-            bool fit_next = false, nan_next = false;
-            int after = -1;
-            if (nxt >= 0) {
-                put(nxt, buf ^ 1, fit_next, nan_next);
-                if (left) {
-                    after = static_cast<int>(__builtin_ctzll(left));
-                    left &= left - 1;
-                    raw.load(part(after), wave, m, g);
-                }
-            }
-            if (!idle) {
-                const u32x4* const page = pages + buf * kFrags * 64 + lane;
-                f32x4 sc[kTiles][4];
-                // the next tile's keys are on their way while one is multiplied
-                u32x4 kf[2][kSteps];
+        f32x4 sc[kTiles][4];
+        float top[kTiles];
+        const auto fetch = [&](const u32x4* keys, int tt, u32x4 (&kf)[kSteps]) {
 #pragma unroll
-                for (int kk = 0; kk < kSteps; ++kk) kf[0][kk] = page[kk * 64];
+            for (int kk = 0; kk < kSteps; ++kk) kf[kk] = keys[(tt * kSteps + kk) * 64 + lane];
+        };
+        // scores of 16 keys
+        const auto scores = [&](const u32x4 (&kf)[kSteps], int tt) {
 #pragma unroll
-                for (int tt = 0; tt < 4; ++tt) {
-                    if (tt < 3)
+            for (int i = 0; i < kTiles; ++i) sc[i][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int kk = 0; kk < kSteps; ++kk) kf[(tt + 1) % 2][kk] = page[((tt + 1) * kSteps + kk) * 64];
+            for (int kk = 0; kk < kSteps; ++kk)
 #pragma unroll
-                    for (int i = 0; i < kTiles; ++i) sc[i][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int x = 0; x < kTerms; ++x)
 #pragma unroll
-                    for (int kk = 0; kk < kSteps; ++kk)
+                    for (int i = 0; i < kTiles; ++i) sc[i][tt] = mfma(kf[kk], col.qf[i][x][kk], sc[i][tt]);
+        };
 #pragma unroll
-                        for (int x = 0; x < kTerms; ++x)
+        for (int tt = 0; tt < 4; ++tt) {
+            u32x4 kf[kSteps];
+            fetch(pages, tt, kf);
+            scores(kf, tt);
+        }
+        largest<kTiles>(sc, top);
+        __syncthreads();
+        for (bool more = true; more;) {
+            u32x4* const page = pages + bit * kFrags * 64;
+            u32x4* const other = pages + (bit ^ 1) * kFrags * 64;
+            raise_reference<D, kTiles>(top, scale, acc);
+            u32x4 w[2][kTiles][kParts], kf[2][kSteps];
+            float base[kTiles];
 #pragma unroll
-                            for (int i = 0; i < kTiles; ++i) sc[i][tt] = mfma(kf[tt % 2][kk], col.qf[i][x][kk], sc[i][tt]);
-                }
-                if constexpr (!kUsual) {
-                    const int row0 = (e0 + cur) * kPageRows;
-                    int seen[kTiles];
+            for (int i = 0; i < kTiles; ++i) base[i] = acc.m[i] == -INFINITY ? 0.f : acc.m[i];
+            fetch(other, 0, kf[0]);
 #pragma unroll
-                    for (int i = 0; i < kTiles; ++i) seen[i] = inside ? col.pos[i] - row0 : kPageRows;
-                    hide_rows<kTiles>(seen, g, sc);
-                    if (nan) {
-                        Values<D> v;
-                        load_values<D, 0>(part(cur), m, g, v);
-                        cut_rows(v.s, g, __builtin_amdgcn_readlane(mine.rows, cur));
-                        poison |= nan_reached<D, kTiles>(v, m, g, seen);
+            for (int tt = 0; tt < 4; ++tt) {
+                if (tt > 0) fetch(other, tt, kf[tt % 2]);
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i) {
+                    float pv[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        pv[x] = __builtin_amdgcn_exp2f(fmaf(sc[i][tt][x], scale, -base[i]));
+                        acc.l[i] += pv[x];
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        if constexpr (kHalf) {
+                            w[tt / 2][i][0][2 * (tt % 2) + y] = pack2h(pv[2 * y], pv[2 * y + 1]);
+                        } else {
+                            uint32_t of[kParts];
+                            split2<kParts>(pv[2 * y], pv[2 * y + 1], of);
+#pragma unroll
+                            for (int x = 0; x < kParts; ++x) w[tt / 2][i][x][2 * (tt % 2) + y] = of[x];
+                        }
                     }
                 }
-                raise_reference<D, kTiles>(sc, scale, acc);
-                const auto values = [&](auto half, auto terms) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-                        half_page<D, decltype(half)::value, decltype(terms)::value, kTiles>(u, sc, scale, [&](auto j, u32x4& even, u32x4& odd) {
-                            const u32x4* from = page + (4 * kSteps + (u * kSteps + decltype(j)::value) * 2) * 64;
-                            even = from[0];
-                            odd = from[64];
-                        }, acc);
-                };
-                if constexpr (kUsual)
-                    values(std::bool_constant<sizeof(T) == 2>(), std::integral_constant<int, sizeof(T) == 2 ? 1 : 3>());
-                else
-                    by_terms<T>(fit, values);
+                // the next page's scores take the registers of those that have just become weights
+                if (tt > 0) scores(kf[(tt + 1) % 2], tt - 1);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            u32x4 vf[2][2];
+            const auto fetch_values = [&](int i, u32x4 (&f)[2]) {
+                f[0] = page[(4 * kSteps + 2 * i) * 64 + lane];
+                f[1] = page[(4 * kSteps + 2 * i + 1) * 64 + lane];
+            };
+            fetch_values(0, vf[0]);
+            scores(kf[1], 3);
+            range.add(vs);
+            __builtin_amdgcn_sched_barrier(0);
+            each(std::make_integer_sequence<int, 2 * kSteps>(), [&](auto at) {
+                constexpr int i = decltype(at)::value, u = i / kSteps, j = i % kSteps;
+                if constexpr (i + 1 < 2 * kSteps) fetch_values(i + 1, vf[(i + 1) % 2]);
+#pragma unroll
+                for (int x = 0; x < kParts; ++x)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) {
+                            f32x4& o = acc.o[t][2 * j + y];
+                            o = kHalf ? mfma_f16(vf[i % 2][y], w[u][t][x], o) : mfma(vf[i % 2][y], w[u][t][x], o);
+                        }
+                // a share of the decoding: keys first
+                if constexpr (i < kSteps)
+                    rk.store(page, wave, lane, i);
+                else if constexpr ((i - kSteps) % 2 == 0 || kSteps == 2)
+                    if constexpr ((i - kSteps) / (kSteps / 2) < RawValues<D>::kPairs)
+                        rv.template store<kHalf, (i - kSteps) / (kSteps / 2)>(vs, other, wave, lane);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            largest<kTiles>(sc, top);
+            more = n1 >= 0;
+            const int n3 = pop();
+            rk.load(part(n3), wave, m, g);
+            rv.load(part(n2), wave, m, g);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) vs[t] = vs_after[t];
+            load_value_scales<D>(part(n3), m, g, vs_after);
+            if (n2 < 0)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) vs[t] = 0x7f7f7f7fu;  // (no page: it fits)
+            n1 = n2;
+            n2 = n3;
+            bit ^= 1;
             __syncthreads();
-            cur = nxt;
-            nxt = after;
-            fit = fit_next;
-            nan = nan_next;
-            buf ^= 1;
-        };
-        // (loops of their own: the rare pages' registers stay out of the others')
-        while (cur >= 0) {
-            while (cur >= 0 && fit && !inside) step(std::true_type());
-            while (cur >= 0 && (!fit || inside)) step(std::false_type());
         }
     }
-    set_nan<D, kTiles>(poison, acc);
+    if (kHalf && !range.fits()) return false;
+    // columns of no token saw the pages too
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+        if (col.pos[i] < 0) {
+            acc.m[i] = -INFINITY;
+            acc.l[i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) acc.o[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
     const int64_t rows = static_cast<int64_t>(tok.n_tokens) * heads;
     put_columns<T, D, kTiles>(a, static_cast<T*>(nullptr), acc, c0, columns, m, g, [&](int c, bool& whole) {
         whole = false;
-        return split * rows + static_cast<int64_t>(at + c / a.ratio) * heads + h * a.ratio + c % a.ratio;
+        return split * rows + static_cast<int64_t>(at_slot + c / a.ratio) * heads + h * a.ratio + c % a.ratio;
     });
+    return true;
 }
 
 // A unit of own pages, sequence by sequence.
@@ -736,8 +819,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shared_kernel(PoolView poo
         if (split >= runs_of(shared, a.run[0], a.most[0])) return;
         if constexpr (kTiles == 0)
             attend_slots<T, D, false, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, u.a, u.b - u.a, shared, split);
-        else
-            attend_wide<T, D, kTiles>(pool, tok, px, a, q, q_stride, smem, where.h, u.a, u.b - u.a, shared, split);
+        else if (!attend_wide<T, D, kTiles>(pool, tok, px, a, q, q_stride, smem, where.h, u.a, u.b - u.a, shared, split)) {
+            // 16 columns at a time
+            const int slots = 16 / a.ratio;
+            for (int at = u.a; at < u.b; at += slots) {
+                __syncthreads();  // LDS is the next columns'
+                attend_slots<T, D, false, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, at, min(slots, u.b - at),
+                                                 shared, split);
+            }
+        }
         return;
     }
     block -= n_group;
@@ -879,7 +969,7 @@ template <typename T, int D, int kTiles>
 hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const PrefixView& px, const SharedArgs& a,
                const void* q, int64_t q_stride, void* out, hipStream_t stream) {
     constexpr size_t kJoin = sizeof(float) * kWaves * 16 * (D + 4 + 2);
-    constexpr size_t kPages = kTiles ? 2 * (D / 4) * 1024 + 3 * kWaves * 4 : 0;
+    constexpr size_t kPages = kTiles ? 2 * (D / 4) * 1024 + 2 * kWaves * 4 : 0;
     constexpr size_t lds = std::max(kJoin, kPages);
     const auto kernel = attend_shared_kernel<T, D, kTiles>;
     hipError_t e;
