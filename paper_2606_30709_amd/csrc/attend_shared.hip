@@ -190,42 +190,60 @@ struct SharedArgs {
     float* part_ml;   // ... and [run][slot][query head][2]: reference, sum
 };
 
-// The group of a slot (each lane its own): of the groups that begin at or before it the last, if the slot is inside it;
-// -1: none.
-__device__ __forceinline__ int group_of(const PrefixView& px, int n_tokens, int slot) {
-    int lo = 0, hi = px.n_groups > 0 ? px.n_groups + 1 : 0;  // begin[0, lo) <= slot < begin[hi, ...)
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (px.begin[mid] <= slot)
-            lo = mid + 1;
-        else
-            hi = mid;
-    }
-    if (lo == 0 || lo > px.n_groups) return -1;
-    return slot >= px.first(lo - 1, n_tokens) && slot < px.end(lo - 1, n_tokens) ? lo - 1 : -1;
-}
-
-// Slots [a, b) of unit `unit` of the groups, and its group; g -1: there is no such unit.
+// Slots [a, b) of a unit of the groups, its group (-1: there is no such unit) and the pages that this shares.
 struct GroupUnit {
-    int g, a, b;
+    int g, a, b, shared;
 };
-__device__ __forceinline__ GroupUnit group_unit(const PrefixView& px, int n_tokens, int slots, int unit) {
+__device__ __forceinline__ GroupUnit group_unit(const PrefixView& px, const TokensView& tok, int slots, int unit) {
     const int lane = threadIdx.x & 63;
     for (int g0 = 0; g0 < px.n_groups; g0 += 64) {
         const int g = g0 + lane;
-        int n = 0;
-        if (g < px.n_groups) n = (px.end(g, n_tokens) - px.first(g, n_tokens) + slots - 1) / slots;
-        const int to = wave_incl_scan_add(n);
+        int a = 0, b = 0, shared = 0;
+        if (g < px.n_groups) {
+            a = px.first(g, tok.n_tokens);
+            b = px.end(g, tok.n_tokens);
+            shared = px.shared(g, tok.max_pages);
+        }
+        const int n = (b - a + slots - 1) / slots, to = wave_incl_scan_add(n);
         const uint64_t past = __builtin_amdgcn_ballot_w64(to > unit);
         if (past) {
             const int l = static_cast<int>(__builtin_ctzll(past));
             const int i = unit - (__builtin_amdgcn_readlane(to, l) - __builtin_amdgcn_readlane(n, l));
-            const int a = px.first(g0 + l, n_tokens) + i * slots;
-            return GroupUnit{g0 + l, a, min(a + slots, px.end(g0 + l, n_tokens))};
+            const int from = __builtin_amdgcn_readlane(a, l) + i * slots;
+            return GroupUnit{g0 + l, from, min(from + slots, __builtin_amdgcn_readlane(b, l)),
+                             __builtin_amdgcn_readlane(shared, l)};
         }
         unit -= __builtin_amdgcn_readlane(to, 63);
     }
-    return GroupUnit{-1, 0, 0};
+    return GroupUnit{-1, 0, 0, 0};
+}
+
+// The groups of slots [from, from + n), n <= 16, a lane each (of the groups that begin at or before a slot the last, if the
+// slot is inside it; -1: none), and the pages that they share.
+struct SlotGroup {
+    int g, shared;
+};
+__device__ __forceinline__ SlotGroup slot_groups(const PrefixView& px, const TokensView& tok, int from, int n) {
+    const int lane = threadIdx.x & 63, slot = from + min(lane, n - 1);
+    int lo = 0, hi = px.n_groups > 0 ? px.n_groups + 1 : 0;  // begin[0, lo) <= slot < begin[hi, ...)
+    if (hi > 0 && hi <= 64) {
+        const int begin = lane < hi ? px.begin[lane] : INT32_MAX;
+        for (int i = 0; i < n; ++i) {
+            const int before = __popcll(__builtin_amdgcn_ballot_w64(begin <= from + i));
+            if (slot == from + i) lo = before;
+        }
+    } else {
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (px.begin[mid] <= slot)
+                lo = mid + 1;
+            else
+                hi = mid;
+        }
+    }
+    if (lo == 0 || lo > px.n_groups || slot < px.first(lo - 1, tok.n_tokens) || slot >= px.end(lo - 1, tok.n_tokens))
+        return SlotGroup{-1, 0};
+    return SlotGroup{lo - 1, px.shared(lo - 1, tok.max_pages)};
 }
 
 __device__ __forceinline__ void add_scaled(float4& o, float f, const float4& x) {
@@ -256,6 +274,15 @@ __device__ __forceinline__ void put4(const SharedArgs& a, T* out, bool whole, in
     }
 }
 
+// The largest of a row of 16 lanes, in all of them.
+template <int kCtrl>
+__device__ __forceinline__ int max_by(int x) {
+    return max(x, __builtin_amdgcn_mov_dpp(x, kCtrl, 0xf, 0xf, true));
+}
+__device__ __forceinline__ int row_max(int x) {
+    return max_by<0x128>(max_by<0x124>(max_by<0x4E>(max_by<0xB1>(x))));  // pairs, quads, then rotations by 4 and 8
+}
+
 // A wavefront's columns: columns c0 + 16 i + m of the slots from `at` on.
 template <typename T, int D, int kTiles>
 struct Columns {
@@ -282,11 +309,12 @@ __device__ __forceinline__ void load_columns(const PoolView& pool, const TokensV
         // columns past the last are no reason to look at rows one by one
         first = min(first, real ? r.pos[i] : INT32_MAX);
         s = in ? max(s, sc) : s;
-        const T* from = q + (in ? t * q_stride : 0) + (static_cast<int64_t>(h) * ratio + c % ratio) * D + g * (D / 4);
+        // (not only if it is in the table: its place need not be known yet)
+        const T* from = q + max(t, 0) * q_stride + (static_cast<int64_t>(h) * ratio + c % ratio) * D + g * (D / 4);
 #pragma unroll
         for (int kk = 0; kk < D / 32; ++kk) {
-            float x[8] = {};
-            if (in) load8(from + 8 * kk, x);
+            float x[8];
+            load8(from + 8 * kk, x);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 uint32_t w[kTerms];
@@ -296,15 +324,9 @@ __device__ __forceinline__ void load_columns(const PoolView& pool, const TokensV
             }
         }
     }
-#pragma unroll
-    for (int x = 1; x < 16; x *= 2) {
-        last = max(last, __shfl_xor(last, x));
-        first = min(first, __shfl_xor(first, x));
-        s = max(s, __shfl_xor(s, x));
-    }
-    r.s = __builtin_amdgcn_readfirstlane(s);
-    r.first = __builtin_amdgcn_readfirstlane(first);
-    r.last = __builtin_amdgcn_readfirstlane(last);
+    r.s = __builtin_amdgcn_readfirstlane(row_max(s));
+    r.first = -1 - __builtin_amdgcn_readfirstlane(row_max(-1 - first));
+    r.last = __builtin_amdgcn_readfirstlane(row_max(last));
 }
 template <int D, int kTiles>
 __device__ __forceinline__ void clear(Acc<D, kTiles>& acc) {
@@ -589,8 +611,7 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
     int s = 0, first = INT32_MAX;  // of the tokens that are some
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) first = min(first, col.pos[i] < 0 ? INT32_MAX : col.pos[i]);
-#pragma unroll
-    for (int x = 1; x < 16; x *= 2) first = min(first, __shfl_xor(first, x));
+    first = -1 - row_max(-1 - first);
     if (lane == 0) {
         s_of[2 * wave] = col.s;
         s_of[2 * wave + 1] = first;
@@ -648,6 +669,9 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
         rv.load(part(n1), wave, m, g);
         load_value_scales<D>(part(n1), m, g, vs);
         load_value_scales<D>(part(n2), m, g, vs_after);
+        if (n1 < 0)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) vs[t] = 0x7f7f7f7fu;  // (no page: it fits)
         __syncthreads();
         f32x4 sc[kTiles][4];
         float top[kTiles];
@@ -749,7 +773,7 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
             load_value_scales<D>(part(n3), m, g, vs_after);
             if (n2 < 0)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) vs[t] = 0x7f7f7f7fu;  // (no page: it fits)
+                for (int t = 0; t < 4; ++t) vs[t] = 0x7f7f7f7fu;
             n1 = n2;
             n2 = n3;
             bit ^= 1;
@@ -782,29 +806,25 @@ __device__ __forceinline__ void attend_own(const PoolView& pool, const TokensVie
     const int lane = threadIdx.x & 63;
     const int from = unit * a.slots[1], n = min(a.slots[1], tok.n_tokens - from);
     // a lane a slot: where a run of slots of one sequence and group begins
-    int group = -1, seq = -1;
-    if (lane < n) {
-        const int t = px.token(from + lane, tok.n_tokens);
-        seq = t < 0 ? -1 : tok.seq[t];
-        group = group_of(px, tok.n_tokens, from + lane);
-        if (t < 0) group = -2;  // no token: a run of its own
-    }
+    const int t = px.token(from + min(lane, n - 1), tok.n_tokens), seq = t < 0 ? -1 : tok.seq[t];
+    const SlotGroup in = slot_groups(px, tok, from, n);
+    const int group = t < 0 ? -2 : in.g;  // no token: a run of its own
     const int seq_before = __shfl_up(seq, 1), group_before = __shfl_up(group, 1);
     const bool begins = lane == 0 || group == -2 || seq != seq_before || group != group_before;
     uint64_t left = __builtin_amdgcn_ballot_w64(lane < n && begins);
     while (left) {
         const int i = static_cast<int>(__builtin_ctzll(left));
         left &= left - 1;
-        const int end = left ? static_cast<int>(__builtin_ctzll(left)) : n, gi = __builtin_amdgcn_readlane(group, i);
+        const int end = left ? static_cast<int>(__builtin_ctzll(left)) : n;
         attend_slots<T, D, true, kAlone>(pool, tok, px, a, q, q_stride, out, smem, h, from + i, end - i,
-                                         gi < 0 ? 0 : px.shared(gi, tok.max_pages), split);
+                                         __builtin_amdgcn_readlane(in.shared, i), split);
         if constexpr (!kAlone) __syncthreads();  // LDS is the next sequence's
     }
 }
 
 // The groups' units first, then the tokens' own pages; a unit's runs stand in the outer order.  kTiles 0: groups of few columns.
 template <typename T, int D, int kTiles>
-__global__ __launch_bounds__(kThreads, 2) void attend_shared_kernel(PoolView pool, TokensView tok, PrefixView px, SharedArgs a,
+__global__ __launch_bounds__(kThreads, (D == 64 && kTiles == 0 ? 3 : 2)) void attend_shared_kernel(PoolView pool, TokensView tok, PrefixView px, SharedArgs a,
                                                                     const T* __restrict__ q, int64_t q_stride,
                                                                     T* __restrict__ out) {
     extern __shared__ __align__(16) float smem[];
@@ -813,9 +833,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shared_kernel(PoolView poo
     if (block < n_group) {
         const int split = static_cast<int>(block / of_group);
         const TokenHead where = token_head(block % of_group, pool.n_kv);
-        const GroupUnit u = group_unit(px, tok.n_tokens, a.slots[0], where.t);
+        const GroupUnit u = group_unit(px, tok, a.slots[0], where.t);
         if (u.g < 0) return;
-        const int shared = px.shared(u.g, tok.max_pages);
+        const int shared = u.shared;
         if (split >= runs_of(shared, a.run[0], a.most[0])) return;
         if constexpr (kTiles == 0)
             attend_slots<T, D, false, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, u.a, u.b - u.a, shared, split);

@@ -55,10 +55,6 @@ __device__ __forceinline__ Sums block_sum(int x, int32_t* s_sum) {
     const int before = wave == 0 ? 0 : __builtin_amdgcn_readlane(to, wave - 1);
     return Sums{before + in - x, total};
 }
-__device__ __forceinline__ uint64_t xor_lane(uint64_t x, int by) {
-    return static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(x), by));
-}
-
 // kHeld: pages of a thread, whose keys it holds; 0: a.per_thread, in a.keys.
 template <int kHeld>
 __global__ __launch_bounds__(kThreads) void choose_kernel(ChooseArgs a, int n_seqs) {
@@ -97,13 +93,22 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(ChooseArgs a, int n_se
             sum[r] = 0.0;
             present[r] = c <= last && static_cast<uint32_t>(table[c]) < static_cast<uint32_t>(a.n_ids);
         }
-        for (int h = 0; h < a.n_kv && last >= 0; ++h) {
-            const float* from = weights + static_cast<int64_t>(h) * a.max_pages;
-            float x[kHeld];
+        // kHeads of a page's words on their way at once (16,384 pages of eight heads, a head at a time: 33 us a call, of which
+        // the loads took 10); a head past the last is the last one again, and is not added
+        constexpr int kHeads = kHeld >= 4 ? 32 / kHeld : 8;
+        for (int h0 = 0; h0 < a.n_kv && last >= 0; h0 += kHeads) {
+            float x[kHeads][kHeld];
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r) x[r] = from[min(r * kThreads + tid, last)];
+            for (int y = 0; y < kHeads; ++y) {
+                const float* from = weights + static_cast<int64_t>(min(h0 + y, a.n_kv - 1)) * a.max_pages;
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r) sum[r] += static_cast<double>(x[r]);
+                for (int r = 0; r < kHeld; ++r) x[y][r] = from[min(r * kThreads + tid, last)];
+            }
+#pragma unroll
+            for (int y = 0; y < kHeads; ++y)
+                if (h0 + y < a.n_kv)
+#pragma unroll
+                    for (int r = 0; r < kHeld; ++r) sum[r] += static_cast<double>(x[y][r]);
         }
 #pragma unroll
         for (int r = 0; r < kHeld; ++r) put(r, present[r], sum[r]);
@@ -141,11 +146,8 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(ChooseArgs a, int n_se
                 most = max(most, k);
             }
         });
-#pragma unroll
-        for (int x = 1; x < 64; x *= 2) {
-            least = min(least, xor_lane(least, x));
-            most = max(most, xor_lane(most, x));
-        }
+        least = ~wave_max_u64(~least);
+        most = wave_max_u64(most);
         __syncthreads();  // the last round's words have been read
         if (lane == 0) {
             s_lo[wave] = least;
