@@ -822,47 +822,50 @@ __device__ __forceinline__ void attend_own(const PoolView& pool, const TokensVie
     }
 }
 
-// The groups' units first, then the tokens' own pages; a unit's runs stand in the outer order.  kTiles 0: groups of few columns.
+// Own pages and groups' pages in one launch; a unit's runs stand in the outer order.  Whose blocks stand first is a matter of
+// which take longer: the tokens' own where the groups' are as short (12 groups of few columns: 24 us the other way round, 21
+// so), the groups' where they are the long ones (16 questions: 559 and 552; drafts 27.6 and 25.9).
+// kTiles 0: groups of few columns.
 template <typename T, int D, int kTiles>
-__global__ __launch_bounds__(kThreads, (D == 64 && kTiles == 0 ? 3 : 2)) void attend_shared_kernel(PoolView pool, TokensView tok, PrefixView px, SharedArgs a,
-                                                                    const T* __restrict__ q, int64_t q_stride,
-                                                                    T* __restrict__ out) {
+__global__ __launch_bounds__(kThreads, (D == 64 && kTiles == 0 ? 3 : 2)) void attend_shared_kernel(
+    PoolView pool, TokensView tok, PrefixView px, SharedArgs a, const T* __restrict__ q, int64_t q_stride, T* __restrict__ out) {
     extern __shared__ __align__(16) float smem[];
     uint32_t block = linear_block<kThreads>();
+    const uint32_t of_own = static_cast<uint32_t>(a.units[1]) * pool.n_kv;
+    const uint32_t n_own = a.alone ? (of_own + kWaves - 1) / kWaves : of_own * a.most[1];
     const uint32_t of_group = static_cast<uint32_t>(a.units[0]) * pool.n_kv, n_group = of_group * a.most[0];
-    if (block < n_group) {
-        const int split = static_cast<int>(block / of_group);
-        const TokenHead where = token_head(block % of_group, pool.n_kv);
-        const GroupUnit u = group_unit(px, tok, a.slots[0], where.t);
-        if (u.g < 0) return;
-        const int shared = u.shared;
-        if (split >= runs_of(shared, a.run[0], a.most[0])) return;
-        if constexpr (kTiles == 0)
-            attend_slots<T, D, false, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, u.a, u.b - u.a, shared, split);
-        else if (!attend_wide<T, D, kTiles>(pool, tok, px, a, q, q_stride, smem, where.h, u.a, u.b - u.a, shared, split)) {
-            // 16 columns at a time
-            const int slots = 16 / a.ratio;
-            for (int at = u.a; at < u.b; at += slots) {
-                __syncthreads();  // LDS is the next columns'
-                attend_slots<T, D, false, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, at, min(slots, u.b - at),
-                                                 shared, split);
-            }
+    constexpr bool kOwnFirst = kTiles == 0;
+    const bool own = kOwnFirst ? block < n_own : block >= n_group;
+    if (own != kOwnFirst) block -= kOwnFirst ? n_own : n_group;
+    if (block >= (own ? n_own : n_group)) return;
+    if (own) {
+        if (a.alone) {
+            // (one run a unit)
+            const uint32_t item = block * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            if (item >= of_own) return;
+            const TokenHead where = token_head(item, pool.n_kv);
+            attend_own<T, D, true>(pool, tok, px, a, q, q_stride, out, smem, where.h, where.t, 0);
+        } else {
+            const TokenHead where = token_head(block % of_own, pool.n_kv);
+            attend_own<T, D, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, where.t,
+                                    static_cast<int>(block / of_own));
         }
         return;
     }
-    block -= n_group;
-    const uint32_t of_own = static_cast<uint32_t>(a.units[1]) * pool.n_kv;
-    if (a.alone) {
-        // (one run a unit)
-        const uint32_t item = block * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (item >= of_own) return;
-        const TokenHead where = token_head(item, pool.n_kv);
-        attend_own<T, D, true>(pool, tok, px, a, q, q_stride, out, smem, where.h, where.t, 0);
-    } else {
-        const int split = static_cast<int>(block / of_own);
-        if (split >= a.most[1]) return;
-        const TokenHead where = token_head(block % of_own, pool.n_kv);
-        attend_own<T, D, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, where.t, split);
+    const int split = static_cast<int>(block / of_group);
+    const TokenHead where = token_head(block % of_group, pool.n_kv);
+    const GroupUnit u = group_unit(px, tok, a.slots[0], where.t);
+    if (u.g < 0 || split >= runs_of(u.shared, a.run[0], a.most[0])) return;
+    if constexpr (kTiles == 0) {
+        attend_slots<T, D, false, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, u.a, u.b - u.a, u.shared, split);
+    } else if (!attend_wide<T, D, kTiles>(pool, tok, px, a, q, q_stride, smem, where.h, u.a, u.b - u.a, u.shared, split)) {
+        // 16 columns at a time
+        const int slots = 16 / a.ratio;
+        for (int at = u.a; at < u.b; at += slots) {
+            __syncthreads();  // LDS is the next columns'
+            attend_slots<T, D, false, false>(pool, tok, px, a, q, q_stride, out, smem, where.h, at, min(slots, u.b - at),
+                                             u.shared, split);
+        }
     }
 }
 
