@@ -624,7 +624,8 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
     }
     s = __builtin_amdgcn_readfirstlane(s);
     first = __builtin_amdgcn_readfirstlane(first);
-    const PageRun run = page_run(split, shared, a.run[0], a.most[0]);
+    PageRun run = page_run(split, shared, a.run[0], a.most[0]);
+    if (first == INT32_MAX) run.b = run.a;  // no token: no row of the table either
     if (first < run.b * kPageRows - 1) return false;
 
     Acc<D, kTiles> acc;

@@ -48,27 +48,31 @@ def attend(sc, batch, px, q, workspace=True, stream=None):
     return out, lse
 
 
-def check_attend(sc, q, got, tokens=slice(None)):
-    """Against the definition of attention over each token's own row.  Bounds as
-    attend_tolerance's, but for bf16's weights, which enter as f16: 2^-11 of each
-    for their rounding, and 2^-34 of the column's largest (two waves' share of
-    2^-35) where that is more -- of the sum of a token's |v| in all, for the
-    weights come to at least the largest."""
-    out, lse = got
-    k, v = sc.k_v()
-    ref, rlse, mag, reach, count = U.attend(f64(q)[tokens], k, v, sc.table, sc.seq[tokens], sc.pos[tokens], sc.kv, None,
-                                            sc.n_ids)
-    one = 1 if sc.dtype == "bf16" else 0
+def attend_tolerance(sc, ref, mag, reach, count, v, seq, pos):
+    """Bounds as tokens_util.attend_tolerance's, but for bf16's weights, which
+    enter as f16: 2^-11 of each for their rounding, and 2^-34 of the column's
+    largest (two waves' share of 2^-35) where that is more -- of the sum of a
+    token's |v| in all, for the weights come to at least the largest."""
     tol, ltol = U.attend_tolerance(sc.dtype, sc.d, ref, mag, reach, count)
-    if one:
+    if sc.dtype == "bf16":
         exact = U.attend_tolerance("f32", sc.d, ref, mag, reach, count)[0]
         every = np.zeros_like(ref)
-        for t, (s, p) in enumerate(zip(sc.seq[tokens], sc.pos[tokens])):
+        for t, (s, p) in enumerate(zip(seq, pos)):
             if not count[t].any():
                 continue
             ids = [i for i in sc.table[s, :p // PAGE + 1] if 0 <= i < sc.n_ids]
             every[t] = np.abs(np.nan_to_num(v[ids])).sum((0, 2)).repeat(sc.hq // sc.kv, 0)
         tol = exact + 2.0 ** -11 * mag + 2.0 ** -8 * np.abs(ref) + 2.0 ** -34 * every
+    return tol, ltol
+
+
+def check_attend(sc, q, got, tokens=slice(None)):
+    """Against the definition of attention over each token's own row."""
+    out, lse = got
+    k, v = sc.k_v()
+    seq, pos = sc.seq[tokens], sc.pos[tokens]
+    ref, rlse, mag, reach, count = U.attend(f64(q)[tokens], k, v, sc.table, seq, pos, sc.kv, None, sc.n_ids)
+    tol, ltol = attend_tolerance(sc, ref, mag, reach, count, v, seq, pos)
     o, l = f64(out)[tokens], f64(lse)[tokens]
     none = count == 0
     assert (o[none] == 0).all() and (l[none] == -np.inf).all()
