@@ -1,7 +1,8 @@
 """Sequences in the pages of a cache: allocation, sharing, copying, moving.
 
 ``PageBook`` is the host's part: which page holds which chunk of which
-sequence, how many sequences share a page, which pages are free.  It touches no
+sequence, how many sequences share a page and which begin with the same pages,
+which pages are free.  It touches no
 device.  ``PagedCache`` keeps a pool and a page table on the GPU in step with
 it, with ``hga_copy_pages`` for what has to move, whichever device is current.
 
@@ -152,6 +153,59 @@ class PageBook:
         for c in range(begin, end):
             self._set(s, c, -1)
 
+    def evict(self, s: int, chunks):
+        """The given full chunks of sequence s become absent, as by drop."""
+        s = self._seq(s)
+        chunks = [int(c) for c in chunks]
+        for c in chunks:
+            self._full(s, c, c + 1)
+        for c in chunks:
+            self._set(s, c, -1)
+
+    def groups(self, seqs):
+        """Which of the given sequences begin with the same pages, as (sequences,
+        pages) of each group of two or more, in the order given: grouped so that the most pages are
+        read once instead of by each.  Only pages full in all of a group count (so
+        that no later append gives one of them a page of its own); absent ones of
+        all count as the same."""
+        seqs = [self._seq(s) for s in seqs]
+        if len(set(seqs)) != len(seqs):
+            raise ValueError("groups: a sequence stands twice")
+        full = {s: int(self.length[s]) // PAGE for s in seqs}
+        # Nodes: sequences that are alike up to `shared`, and then go apart.  If a group is formed at a node, its
+        # sequences that no deeper group takes save `shared` pages each, but for one of them.  above: what a sequence
+        # saves in a group of one of the nodes above (0: in none).
+        nodes, todo = [], [(seqs, 0, -1, np.zeros(1, np.int64))]
+        while todo:
+            members, at, parent, above = todo.pop()
+            rows = self.table[members, at:min((full[s] for s in members), default=0)]
+            differ = np.nonzero((rows != rows[:1]).any(0))[0]
+            shared = at + (int(differ[0]) if len(differ) else rows.shape[1])
+            parts: dict = {}
+            for s in members:
+                parts.setdefault(int(self.table[s, shared]) if full[s] > shared else ~s - 1, []).append(s)
+            own = [p[0] for p in parts.values() if len(p) == 1]
+            below = np.append(above, shared)
+            todo += [(p, shared, len(nodes), below) for p in parts.values() if len(p) > 1]
+            nodes.append([own, shared, parent, above, len(own) * below, None])
+        for node in reversed(nodes):    # the pages saved, with a group here and without
+            _, shared, parent, _, saved, _ = node
+            node[5] = saved[-1] - shared > saved[:-1]
+            if parent >= 0:
+                nodes[parent][4] = nodes[parent][4] + np.maximum(saved[-1] - shared, saved[:-1])
+        result, taken = [], []          # the group that a node's sequences are in, and its place in `above`
+        for own, shared, parent, above, _, better in nodes:
+            group, place = taken[parent] if parent >= 0 else (None, 0)
+            if better[place]:
+                group, place = ([], shared), len(above)
+                result.append(group)
+            taken.append((group, place))
+            if group is not None:
+                group[0].extend(own)
+        rank = {s: i for i, s in enumerate(seqs)}
+        return sorted(((sorted(members, key=rank.get), shared) for members, shared in result),
+                      key=lambda g: rank[g[0][0]])
+
     def move(self, s: int, begin: int, end: int, cold: bool):
         """The pages of full chunks [begin, end) of sequence s go to the cold
         tier, or back, for every sequence that shares them."""
@@ -233,6 +287,59 @@ class PagedCache:
         tok[1] = np.arange(n) - np.repeat(np.cumsum(counts) - counts, counts) + np.repeat(start, counts)
         tok = self._upload(tok)
         return hga.TokenBatch(tok[0], tok[1], self.page_table)
+
+    def prefixes(self, batch: hga.TokenBatch, seqs, counts) -> hga.Prefixes | None:
+        """What the batch that ``append(seqs, counts)`` gave shares, for
+        hga_attend_shared (None: nothing).  It stays valid for batches of the same
+        counts while their sequences only grow or move (``to_cold``, ``to_device``,
+        ``compact``); a sequence of it that is cut, dropped from, evicted from,
+        forked over or released needs another one.  Its hints are those of the
+        lengths now."""
+        seqs, counts = np.asarray(seqs, np.int64).reshape(-1), np.asarray(counts, np.int64).reshape(-1)
+        if int(counts.sum()) != batch.n_tokens:
+            raise ValueError(f"prefixes: {int(counts.sum())} tokens, the batch has {batch.n_tokens}")
+        some = counts > 0
+        groups = self.book.groups(seqs[some].tolist())
+        if not groups:
+            return None
+        start = dict(zip(seqs.tolist(), (np.cumsum(counts) - counts).tolist()))
+        n = dict(zip(seqs.tolist(), counts.tolist()))
+        pages = {s: p for members, p in groups for s in members}
+        slots = [t for members, _ in groups for s in members for t in range(start[s], start[s] + n[s])]
+        alone = [t for s in seqs[some].tolist() if s not in pages for t in range(start[s], start[s] + n[s])]
+        begin = np.cumsum([0] + [sum(n[s] for s in members) for members, _ in groups])
+        own = max(-(-int(self.book.length[s]) // PAGE) - pages.get(s, 0) for s in seqs[some].tolist())
+        up = self._upload(np.concatenate((slots, alone, begin, [p for _, p in groups])).astype(np.int32))
+        # (the calls ask for alignment to four bytes alone)
+        order, begin, shared = up.split((batch.n_tokens, len(groups) + 1, len(groups)))
+        return hga.Prefixes(order, begin, shared, max(p for _, p in groups), max(own, 1))
+
+    def evict(self, weights: torch.Tensor, budget) -> list:
+        """Drop of each sequence s the pages above budget[s] (an int: of every one)
+        that hga_choose_evictions names by ``weights`` (fp32 [n_seqs, n_kv_heads,
+        max_pages]: those of one layer, or a sum over them); the chunks dropped,
+        a list for each sequence.  Waits for the device; the weights are not
+        changed (an absent page gets nothing more)."""
+        book = self.book
+        n_seqs = len(book.length)
+        want = np.broadcast_to(np.asarray(budget, np.int64), (n_seqs,))
+        here = (book.table >= 0).sum(1)
+        most = int((here - want).clip(0).max(initial=0))
+        if most == 0:
+            return [[] for _ in range(n_seqs)]
+        dev = self.pool.device
+        with torch.cuda.device(self.pool.index):
+            state = self._upload(np.stack((book.length, want.clip(0, 2 ** 31 - 1))).astype(np.int32))
+            out = torch.empty(n_seqs, most, dtype=torch.int32, device=dev)
+            nbytes = hga.hga_choose_evictions_workspace(self.plan, self.page_table)
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+            hga.hga_choose_evictions(self.plan, self.page_table, book.n_pages + book.n_cold, state[0], weights,
+                                     state[1], out, workspace=ws)
+            chosen = [[c for c in row if c >= 0] for row in out.tolist()]
+        for s, chunks in enumerate(chosen):
+            book.evict(s, chunks)
+        self._apply(None)
+        return chosen
 
     def truncate(self, s: int, length: int):
         """As PageBook.truncate; so the methods that follow."""

@@ -25,7 +25,8 @@ results are identical.
 
 ``TokenPipeline``: single tokens of any sequences over a paged 4-bit cache
 (``pages.PagedCache``); one step appends a layer's rows, routes each token and
-attends it over its own pages.
+attends it over its own pages (or, unrouted, over all of them, those that
+sequences share once for all), and can weigh the pages for an eviction.
 
 The pipelines only allocate with torch and call the binding; all arithmetic runs
 in the HIP library.
@@ -529,7 +530,8 @@ class DecodeSequencePipeline:
 class TokenPipeline:
     """One layer's attention of a batch of tokens over a ``PagedCache``: their
     rows appended, each token routed to its own chunks (or, with ``routed``
-    false, given all of them) and attended.  Buffers are those of the largest
+    false, given all of them, pages that sequences share read once) and attended;
+    if asked, what each page got of the attention added to its weight.  Buffers are those of the largest
     batch so far, so that a step of a size seen before allocates nothing and
     may be captured into a graph; one that would have to allocate is refused
     while a stream captures.  What a captured step uses is kept for the
@@ -558,26 +560,43 @@ class TokenPipeline:
             self._captured[t.data_ptr()] = t
         return t[:n].view(shape)
 
-    def step(self, layer: int, batch: hga.TokenBatch, q, k, v):
+    def step(self, layer: int, batch: hga.TokenBatch, q, k, v, prefixes: hga.Prefixes | None = None,
+             weights: torch.Tensor | None = None):
         """q [n_tokens, n_q_heads, d], k and v [n_tokens, n_kv_heads, d]; returns
         out (as q) and lse fp32 [n_tokens, n_q_heads], valid until the next
-        step.  Runs on the current stream."""
+        step.  prefixes (``PagedCache.prefixes``; without routing): the pages
+        that the batch's sequences share.  weights fp32 [n_seqs, n_kv_heads,
+        max_pages]: the pages' attention weight, added to (``PagedCache.evict``
+        takes it).  Runs on the current stream."""
         p, plan, pool = self.plan.params, self.plan, self.cache.pool
         T = batch.n_tokens
         # every buffer before the first launch
         out = self._buffer("out", (T, p.n_q_heads, p.head_dim), plan.torch_dtype)
         lse = self._buffer("lse", (T, p.n_q_heads), torch.float32)
-        lists = route = attend = None
+        lists = route = attend = weigh = None
+        if self.routed and prefixes is not None:
+            raise hga.HgaError(-1, "HGA_EINVAL: routed tokens see pages of their own each: no prefixes")
         if self.routed:
             lists = self._buffer("lists", (T, p.n_kv_heads, hga.hga_token_list_size(plan)),
                                  torch.int32)
             nbytes = hga.hga_route_tokens_workspace(plan, batch)
             route = self._buffer("route", (nbytes,), torch.uint8) if nbytes else None
-        nbytes = hga.hga_attend_tokens_workspace(plan, batch, lists)
+        nbytes = (hga.hga_attend_tokens_workspace(plan, batch, lists) if prefixes is None else
+                  hga.hga_attend_shared_workspace(plan, batch, prefixes))
         attend = self._buffer("attend", (nbytes,), torch.uint8) if nbytes else None
+        if weights is not None:
+            nbytes = hga.hga_weigh_pages_workspace(plan, batch, lists)
+            weigh = self._buffer("weigh", (nbytes,), torch.uint8) if nbytes else None
         hga.hga_cache_append(plan, pool, layer, batch, k, v)
         if self.routed:
             hga.hga_route_tokens(plan, pool, layer, batch, q, lists, workspace=route)
-        hga.hga_attend_tokens(plan, pool, layer, batch, q, out, lse=lse, chunk_list=lists,
-                              workspace=attend)
+        if prefixes is None:
+            hga.hga_attend_tokens(plan, pool, layer, batch, q, out, lse=lse, chunk_list=lists,
+                                  workspace=attend)
+        else:
+            hga.hga_attend_shared(plan, pool, layer, batch, prefixes, q, out, lse=lse,
+                                  workspace=attend)
+        if weights is not None:
+            hga.hga_weigh_pages(plan, pool, layer, batch, q, lse, weights, prev=weights,
+                                chunk_list=lists, workspace=weigh)
         return out, lse
