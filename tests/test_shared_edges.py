@@ -107,6 +107,42 @@ def test_values_beyond_sixteen_bits(hga, dtype, d, kv, ratio, n, low, high):
 
 
 @pytest.mark.parametrize("dtype,d,kv,ratio,n", SHAPES)
+@pytest.mark.parametrize("low,high", [(109, 112), (109, 141), (137, 141), (108, 110)])
+def test_values_at_the_ends_of_sixteen_bits(hga, dtype, d, kv, ratio, n, low, high):
+    """All values as small, or as large, as f16 holds them (its subnormals among
+    them): a value that is lost there would be all of a result."""
+    pages = 11
+    sc = _group(hga, dtype, d, kv, ratio, n, pages, seed=n + low)
+    first = PAGE * (d + d // 32)
+    sc.bytes[..., first:] = sc.rng.integers(low, high, sc.bytes[..., first:].shape)
+    _upload(sc)
+    seq = np.arange(n + 1)
+    batch = sc.batch(seq, [sc.lens[s] - 1 for s in seq])
+    q = sc.random(n + 1, sc.hq, d)
+    px = P.prefixes(hga, seq, {s: 0 for s in range(n)}, [pages], sc.rng)
+    P.check_attend(sc, q, P.attend(sc, batch, px, q))
+
+
+@pytest.mark.parametrize("dtype,d,kv,ratio", [("bf16", 128, 2, 8), ("f32", 64, 1, 2), ("bf16", 64, 3, 1)])
+def test_groups_of_very_different_sizes(hga, dtype, d, kv, ratio):
+    """One large group among small ones and the other way round; prefixes of one
+    page and of many."""
+    for sizes, pages in (((70, 1, 2, 1, 3, 2, 2, 1), (9, 1, 40, 2, 3, 66, 5, 1)), ((1, 90, 1), (70, 20, 1)), ((2,) * 70, (3,) * 70)):
+        lens, groups, at = [], [], 0
+        for m, p in zip(sizes, pages):
+            lens += [PAGE * p + 1 + 13 * i % 200 for i in range(m)]
+            groups.append((at, list(range(at + 1, at + m)), p))
+            at += m
+        sc = Scene(hga, dtype, d, kv, ratio, lens=lens, seed=len(sizes))
+        P.share(sc, groups)
+        seq = sc.rng.permutation(at)
+        batch = sc.batch(seq, [lens[s] - 1 for s in seq])
+        q = sc.random(at, sc.hq, d)
+        of = {s: g for g, (a, more, _) in enumerate(groups) for s in [a, *more]}
+        P.check_attend(sc, q, P.attend(sc, batch, P.prefixes(hga, seq, of, list(pages), sc.rng), q))
+
+
+@pytest.mark.parametrize("dtype,d,kv,ratio,n", SHAPES)
 def test_long_prefixes_with_absent_stretches(hga, dtype, d, kv, ratio, n):
     """Prefixes of a page more than 64, 128; more than 64 absent pages in a row;
     single pages between absent ones; any number of runs."""
