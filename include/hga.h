@@ -755,9 +755,10 @@ hga_status hga_copy_pages(const hga_plan* plan, const hga_pool* pool, const int3
  * group's pages: it sees them up to its position.
  *   shared_hint, own_hint  the largest of group_pages, and the most pages that a
  *               token has behind its group's, as far as the host knows; 0: it
- *               does not.  They say how the work is cut: results are right, up
- *               to the order of sums, whatever they are (a captured call keeps
- *               them).
+ *               does not (then as many as the table is wide).  They say whether
+ *               and how the work is shared out: results are right, up to the
+ *               order of sums and the weights' rounding, whatever they are (a
+ *               captured call keeps them).
  * What is read of the device arrays is checked by the kernels: words that are
  * none of this lead to results of any value, never outside the call's arrays. */
 typedef struct {
@@ -776,8 +777,11 @@ int64_t hga_attend_shared_workspace(const hga_plan* plan, int32_t n_tokens, int3
                                     int32_t own_hint);
 
 /* hga_attend_tokens over whole histories, each group's shared pages read once:
- * out and lse are what that call writes, up to the order of sums.  Arguments,
- * requirements and errors as there, without lists;
+ * out and lse are what that call writes, up to the order of sums and, in bf16,
+ * the rounding of the weights (to 11 bits here, a 2^-12 of each; to 16 there).
+ * Where groups are so small, or share so little, that this takes longer than each
+ * token by itself, it is that call.  Arguments, requirements and errors as there,
+ * without lists;
  *   workspace   hga_attend_shared_workspace bytes; with fewer the work is cut
  *               into fewer runs, and below a partial result each of the
  *               groups' and the tokens' own pages nothing is shared (NULL and

@@ -1,9 +1,16 @@
 // Attention of a batch whose sequences share leading pages (Sec. 3.4 at the token's grain): the shared pages are read and
-// multiplied once for many tokens, each token's own pages by itself, and the two are joined.
+// multiplied once for many tokens, each token's own pages by itself, and the two are joined.  With keys o of the shared pages
+// and o' of the own ones, m a reference near the largest score, l = sum exp(s - m), O = sum exp(s - m) v:
+//   out = (e O + e' O') / (e l + e' l'),  e = exp(m - M), e' = exp(m' - M), M = max(m, m'),  lse = M + log(e l + e' l').
 //
-// A unit is one KV head and up to 16 kTiles / r slots: of one group, over its shared pages, or of one sequence, over the
-// pages behind them.  Its query heads are the columns of the tiles, as in the attention of single tokens (attend_pages.hpp);
-// a unit's pages are cut into runs, a workgroup each, whose partial results a second kernel joins in order.
+// A unit is one KV head and the slots that fill its tiles with columns, a column a query head (attend_pages.hpp): of one
+// group, over its shared pages, or of one sequence, over the pages behind them.  Groups of few columns: a tile a workgroup,
+// whose wavefronts take pages in turns and decode each for itself.  Of many: a workgroup's wavefronts hold columns of their
+// own (4 times 32, or 16 in fp32 at 128 dimensions) and decode each page once for all of them, into LDS.  A unit's pages are cut into runs, a workgroup
+// each, so that some 512 are at work; a second kernel joins the runs' results in order.
+//
+// 64 samples of a 16K prompt (32/4 heads d128 bf16): 48 us; 16 questions of 128 tokens about 16K: 545 us (1.0 PFLOP/s; 1.9 us
+// a page, 1.14 PFLOP/s, as fast as a large matrix product here).
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -383,7 +390,7 @@ __device__ __forceinline__ void put_columns(const SharedArgs& a, T* out, const A
 }
 
 // Up to 16 columns of one group (over its shared pages, [0, shared)) or of one sequence (over its own, from `shared` on):
-// their queries against run `split` of the pages, which n_waves wavefronts take in turns and join (n_waves 1: this one by
+// their queries against run `split` of the pages, which the workgroup's wavefronts take in turns and join (kAlone: this one by
 // itself, without a barrier).
 template <typename T, int D, bool kOwn, bool kAlone>
 __device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensView& tok, const PrefixView& px,
@@ -591,7 +598,11 @@ __device__ __forceinline__ void load_value_scales(buf_rsrc r, int m, int g, uint
 
 // Many columns of one group, kTiles tiles a wavefront, against run `split` of its pages.  The wavefronts decode a page once,
 // a share each, into LDS.  A page's weights are formed beside the products of the next one's keys, and its values are
-// multiplied beside the decoding of further pages, so that neither unit of a SIMD waits for the other.
+// multiplied beside the decoding of further pages, so that neither unit of a SIMD waits for the other: a wavefront issues
+// some 64 products (1,024 cycles of the matrix unit), 170 vector instructions and 32 exponentials a page, two wavefronts a
+// SIMD.  16 questions of 128 tokens after 16K: 814 us with each wavefront decoding for itself, 640 through LDS, 583 with what
+// is rare outside the loop (its registers made the loop spill), 543 with the products beside the weights.  Four tiles a
+// wavefront, one wavefront a SIMD: 1,777 (spills); eight wavefronts to a page: 607 (a barrier's phases meet).
 // Only for columns that see all of the run, and for a bf16 call values that fit f16; false: they do not, nothing is stored.
 template <typename T, int D, int kTiles>
 __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensView& tok, const PrefixView& px,
@@ -934,7 +945,7 @@ __global__ __launch_bounds__(256) void join_shared_kernel(int n_tokens, int head
     put4<T, D>(a, out, true, static_cast<int64_t>(t) * heads + head, 4 * col, o, m, l);
 }
 
-// How a call is cut: columns of a tile row, slots of a unit, pages of a run and runs of a unit at most, units; [0] the groups'
+// How a call is cut: slots of a unit, pages of a run and runs of a unit at most, units; [0] the groups'
 // pages, [1] the tokens' own.
 struct Cut {
     int tiles;  // of a wavefront of a group's unit; 0: the unit is one tile, for few columns
@@ -945,6 +956,23 @@ struct Cut {
 
 int64_t pad16(int64_t n) { return (n + 15) / 16 * 16; }
 
+// Tiles of a wavefront of a group's unit; 0: a tile a workgroup, which needs a shorter start and finds more workgroups to run
+// beside it.  Several where a group has the columns (on average) and all tiles have pages to multiply for some 70 us: us with
+// one tile and with several, 32/4 heads d128 bf16: 32K tile pages (64 samples of 256 pages) 50 and 62, 65K 66 and 67, 131K 123
+// and 102, 524K 406 and 289 (16 questions of 128 tokens after 256: 808 and 535); 8/8 heads d64 bf16, 32K 44 and 49, 131K 114
+// and 81; 16/4 d64 fp32, 65K 84 and 85, 262K 290 and 188; 16/4 d128 fp32, 32K 58 and 61, 131K 177 and 171.  Groups of 32 and
+// 64 columns, 32K tile pages: 26 and 31, 33 and 41.
+int tiles_of(const hga_plan& plan, int n_tokens, int n_groups, int shared_pages) {
+    const int64_t columns = static_cast<int64_t>(n_tokens) * (plan.p.n_q_heads / plan.p.n_kv_heads);
+    if (columns <= 64 * static_cast<int64_t>(n_groups) || columns / 16 * plan.p.n_kv_heads * shared_pages < 3 << 15) return 0;
+    return plan.p.dtype == HGA_F32 && plan.p.head_dim == 128 ? 1 : 2;
+}
+// Slots of a tile of one sequence.
+int own_slots(const hga_plan& plan, int n_tokens, int n_seqs) {
+    const int64_t per_seq = (static_cast<int64_t>(n_tokens) + n_seqs - 1) / std::max(n_seqs, 1);
+    return static_cast<int>(std::clamp<int64_t>(per_seq, 1, 16 / (plan.p.n_q_heads / plan.p.n_kv_heads)));
+}
+
 Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int n_groups, int shared_hint, int own_hint,
              int64_t ws_bytes) {
     const int ratio = plan.p.n_q_heads / plan.p.n_kv_heads, kv = plan.p.n_kv_heads;
@@ -953,12 +981,9 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
     const int64_t cus = plan.n_cu;
     const auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     Cut c{};
-    // by the columns that a group has on average
-    const int64_t columns = static_cast<int64_t>(n_tokens) * ratio / std::max(n_groups, 1);
-    c.tiles = columns <= 16 ? 0 : columns <= 64 || (plan.p.dtype == HGA_F32 && plan.p.head_dim == 128) ? 1 : 2;
+    c.tiles = tiles_of(plan, n_tokens, n_groups, static_cast<int>(pages[0]));
     c.slots[0] = 16 * (c.tiles ? c.tiles * kWaves : 1) / ratio;
-    const int per_seq = static_cast<int>(up(n_tokens, std::max(n_seqs, 1)));
-    c.slots[1] = std::clamp(per_seq, 1, 16 / ratio);
+    c.slots[1] = own_slots(plan, n_tokens, n_seqs);
     // a group's last unit may be a small one
     c.units[0] = n_groups ? static_cast<int>(std::min<int64_t>(n_tokens, n_tokens / c.slots[0] + static_cast<int64_t>(n_groups))) : 0;
     c.units[1] = static_cast<int>(up(n_tokens, c.slots[1]));
@@ -972,7 +997,8 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
         c.run[i] = static_cast<int>(up(pages[i], c.most[i]));
     }
     // Own pages by a wavefront or a workgroup: what a round of workgroups takes, in pages, about five of them for what comes
-    // before the first.
+    // before the first (116 tokens of 8 heads, up to 10 pages: 27 us by wavefronts, 35 by workgroups; 64 of 4, up to 32, by
+    // workgroups 60, by wavefronts 71).
     const int64_t own = static_cast<int64_t>(c.units[1]) * kv;
     c.alone = c.most[1] == 1 && up(own, 2 * kWaves * cus) * (5 + pages[1]) <= up(own, 2 * cus) * (5 + up(pages[1], kWaves));
     const int64_t counts = pad16(static_cast<int64_t>(n_tokens) * 8);
@@ -1031,6 +1057,20 @@ int64_t attend_shared_bytes(const hga_plan& plan, int n_tokens, int n_seqs, int 
     return cut_call(plan, n_tokens, n_seqs, max_pages, n_groups, shared_hint, own_hint, must ? 0 : INT64_MAX).bytes;
 }
 
+// Whether reading shared pages once is worth a second kernel: by the pages that tiles of single sequences would multiply, each
+// as much as prefixes of up to 128 pages are long.  Measured over 1 and 8 groups of 2 to 128 sequences after 8 to 384 pages
+// (32/4 heads d128 and 8/8 d64 bf16, 16/4 d128 and 8/4 d64 fp32; 1 and 4 tokens each), us shared and not: 512 tile pages of
+// prefixes of 8 pages 8.9 and 6.1, 4,096 of 8 19.0 and 13.0, 2,048 of 32 12.1 and 11.5, 4,096 of 32 13.8 and 15.5, 16,384 of 8
+// 14.2 and 22.3, 4,096 of 128 14.2 and 16.4, 16,384 of 128 22.6 and 29.8, 65,536 of 32 20.4 and 51.3; above the border it is
+// longer by 7 us at most (16,384 of 32, drafts of four in fp32: 44.9 and 37.9).
+bool attend_shared_pays(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int n_groups, int shared_hint) {
+    if (n_groups == 0 || std::min(n_seqs, n_tokens) < 2 * static_cast<int64_t>(n_groups)) return false;
+    const int64_t tiles = (static_cast<int64_t>(n_tokens) + own_slots(plan, n_tokens, n_seqs) - 1) / own_slots(plan, n_tokens, n_seqs);
+    const int64_t pages = std::min(shared_hint, max_pages);
+    const int64_t least = 1 << 17;
+    return tiles * plan.p.n_kv_heads * pages * std::min<int64_t>(pages, 128) >= least;
+}
+
 hipError_t launch_attend_shared(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const PrefixView& px,
                                 int shared_hint, int own_hint, const void* q, int64_t q_stride, void* out, float* lse,
                                 void* ws, int64_t ws_bytes, hipStream_t stream) {
@@ -1052,7 +1092,7 @@ hipError_t launch_attend_shared(const hga_plan& plan, const PoolView& pool, cons
     const auto go = [&](auto zero, auto dim) {
         using T = decltype(zero);
         constexpr int D = decltype(dim)::value, kMost = sizeof(T) == 4 && D == 128 ? 1 : 2;
-        const auto f = c.tiles == 0 ? run<T, D, 0> : c.tiles == 1 ? run<T, D, 1> : run<T, D, kMost>;
+        const auto f = c.tiles ? run<T, D, kMost> : run<T, D, 0>;
         return f(plan, pool, tok, px, a, q, q_stride, out, stream);
     };
     const bool f32 = plan.p.dtype == HGA_F32;

@@ -7,6 +7,10 @@
 // then listed in order, placed by the counts of each wavefront's 64 neighbouring pages.
 //
 // Up to 16,384 pages the keys stay in registers; of longer tables they lie in the workspace.
+//
+// Bound by latency, and for long tables by one CU's arithmetic: 2,048 pages of 4 heads 11.5 us (loads 1.0, counts 1.2, two
+// rounds of 2.5, the list 0.9), 8 times 16,384 pages of 8 heads 30 us (loads and sums 7, two or three rounds of 4, the list 3;
+// with the keys in memory 72, with 64-bit shuffles for the ends of the range and a head's weights at a time 33).
 #include <algorithm>
 #include <type_traits>
 
@@ -93,8 +97,8 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(ChooseArgs a, int n_se
             sum[r] = 0.0;
             present[r] = c <= last && static_cast<uint32_t>(table[c]) < static_cast<uint32_t>(a.n_ids);
         }
-        // kHeads of a page's words on their way at once (16,384 pages of eight heads, a head at a time: 33 us a call, of which
-        // the loads took 10); a head past the last is the last one again, and is not added
+        // kHeads of a page's words on their way at once (64 tables of 2,048 pages, eight heads: 13.5 us a call a head at a
+        // time, 11.5 so); a head past the last is the last one again, and is not added
         constexpr int kHeads = kHeld >= 4 ? 32 / kHeld : 8;
         for (int h0 = 0; h0 < a.n_kv && last >= 0; h0 += kHeads) {
             float x[kHeads][kHeld];

@@ -30,8 +30,10 @@ int64_t hga_attend_shared_workspace(const hga_plan* plan, int32_t n_tokens, int3
     if (!plan) return fail(HGA_EINVAL, "plan is NULL");
     HGA_TRY(check_counts(plan, n_tokens, n_seqs, max_pages));
     HGA_TRY(check_groups(plan, n_tokens, n_groups, shared_hint, own_hint));
-    return hga::attend_shared_bytes(*plan, n_tokens, n_seqs, max_pages, n_groups, hint(shared_hint, max_pages),
-                                    hint(own_hint, max_pages), false);
+    const int32_t shared = hint(shared_hint, max_pages), own = hint(own_hint, max_pages);
+    return hga::attend_shared_pays(*plan, n_tokens, n_seqs, max_pages, n_groups, shared)
+               ? hga::attend_shared_bytes(*plan, n_tokens, n_seqs, max_pages, n_groups, shared, own, false)
+               : hga::attend_tokens_bytes(*plan, n_tokens, n_seqs, max_pages, 0);
 }
 
 hga_status hga_attend_shared(const hga_plan* plan, const hga_pool* pool, int32_t layer, const hga_tokens* tokens,
@@ -56,9 +58,11 @@ hga_status hga_attend_shared(const hga_plan* plan, const hga_pool* pool, int32_t
     if (lse) HGA_TRY(check_index(lse, "lse"));
     const int shared = hint(prefixes->shared_hint, tv.max_pages), own = hint(prefixes->own_hint, tv.max_pages);
     clear_stale_error();
-    // without room for a partial result each of the groups' and the tokens' own pages nothing can be shared
-    if (workspace_bytes <
-        hga::attend_shared_bytes(*plan, tv.n_tokens, tv.n_seqs, tv.max_pages, prefixes->n_groups, shared, own, true))
+    // token by token where sharing does not pay, or without room for a partial result each of the groups' and the tokens' own
+    // pages
+    if (!hga::attend_shared_pays(*plan, tv.n_tokens, tv.n_seqs, tv.max_pages, prefixes->n_groups, shared) ||
+        workspace_bytes <
+            hga::attend_shared_bytes(*plan, tv.n_tokens, tv.n_seqs, tv.max_pages, prefixes->n_groups, shared, own, true))
         return launched(hga::launch_attend_tokens(*plan, pv, tv, q, q_stride, nullptr, 0, out, lse, workspace,
                                                   workspace_bytes, static_cast<hipStream_t>(stream)),
                         "hga_attend_shared launch");

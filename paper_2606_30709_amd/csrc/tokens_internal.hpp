@@ -41,10 +41,12 @@ hipError_t launch_attend_tokens(const hga_plan& plan, const PoolView& pool, cons
                                 hipStream_t stream);
 
 // Attention over prefixes that sequences share, the bytes its workspace may
-// take (must: the fewest with which anything is shared), the pages' attention
-// weight, and the choice of pages to evict.
+// take (must: the fewest with which anything is shared), whether it pays, the
+// pages' attention weight, and the choice of pages to evict.
 int64_t attend_shared_bytes(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages,
                             int n_groups, int shared_hint, int own_hint, bool must);
+bool attend_shared_pays(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int n_groups,
+                        int shared_hint);
 hipError_t launch_attend_shared(const hga_plan& plan, const PoolView& pool, const TokensView& tok,
                                 const PrefixView& prefixes, int shared_hint, int own_hint,
                                 const void* q, int64_t q_stride, void* out, float* lse, void* ws,

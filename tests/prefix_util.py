@@ -36,14 +36,32 @@ def prefixes(hga, seq, group_of_seq, pages, rng, shared_hint=None, own_hint=0):
     return hga.Prefixes(i32(order), i32(begin), i32(pages), hint, own_hint)
 
 
-def attend(sc, batch, px, q, workspace=True, stream=None):
+def sharing(sc, batch, px, few=False):
+    """The batch and prefixes with which the call shares whatever there is to
+    share: through a table so wide, its hints unknown, that it looks worth it --
+    and, where groups have more than 64 columns, worth the form for many of them
+    (few: the one for few)."""
+    columns = batch.n_tokens * (sc.hq // sc.kv)
+    width = 600 if batch.n_tokens * sc.kv >= 90 else 4096
+    if columns > 64 * px.n_groups > 0 and not few:
+        width = max(batch.max_pages, -(-(3 << 15) // (columns // 16 * sc.kv)))
+    wide = torch.full((batch.n_seqs, width), -1, dtype=torch.int32, device="cuda")
+    wide[:, :batch.max_pages] = batch.page_table
+    return (sc.hga.TokenBatch(batch.tok_seq, batch.tok_pos, wide),
+            sc.hga.Prefixes(px.order, px.group_begin, px.group_pages, 0, px.own_hint))
+
+
+def attend(sc, batch, px, q, workspace=True, stream=None, share=True):
+    """The call, made to share (True; "few": in the form for few columns) or as
+    it is.  workspace: True, or bytes, or a share of what it asks for."""
     hga = sc.hga
+    if share:
+        batch, px = sharing(sc, batch, px, share == "few")
     out = torch.full((batch.n_tokens, sc.hq, sc.d), float("nan"), dtype=U.DT[sc.dtype], device="cuda")
     lse = torch.full((batch.n_tokens, sc.hq), float("nan"), device="cuda")
-    ws = None
-    if workspace:
-        nb = hga.hga_attend_shared_workspace(sc.plan, batch, px) if workspace is True else workspace
-        ws = torch.full((nb,), 255, dtype=torch.uint8, device="cuda") if nb else None
+    nb = hga.hga_attend_shared_workspace(sc.plan, batch, px)
+    nb = nb if workspace is True else int(nb * workspace) // 16 * 16 if isinstance(workspace, float) else workspace
+    ws = torch.full((nb,), 255, dtype=torch.uint8, device="cuda") if nb else None
     hga.hga_attend_shared(sc.plan, sc.pool, sc.layer, batch, px, q, out, lse=lse, workspace=ws, stream=stream)
     return out, lse
 

@@ -26,6 +26,9 @@ hipError_t launch_attend_tokens(const hga_plan&, const PoolView&, const TokensVi
     ++g_plain;
     return hipSuccess;
 }
+int64_t attend_tokens_bytes(const hga_plan&, int, int, int, int) { return 16; }
+// (a shared_hint of 3: too little)
+bool attend_shared_pays(const hga_plan&, int, int, int, int, int shared) { return shared != 3; }
 int64_t attend_shared_bytes(const hga_plan&, int, int, int, int, int, int, bool must) { return must ? 32 : 64; }
 hipError_t launch_attend_shared(const hga_plan&, const PoolView&, const TokensView& tok, const PrefixView&, int shared, int own,
                                 const void*, int64_t, void*, float*, void*, int64_t, hipStream_t) {
@@ -121,6 +124,9 @@ static void refusals() {
     // without room for two partial results nothing is shared
     EXPECT(attend(0, buf, 256, buf, nullptr, buf, 16) == HGA_OK && attend(0, buf, 256, buf, nullptr, nullptr, 0) == HGA_OK);
     EXPECT(g_plain == 2 && g_launches == 4);
+    px.shared_hint = 3;
+    EXPECT(attend() == HGA_OK && g_plain == 3 && g_launches == 4);
+    EXPECT(hga_attend_shared_workspace(&plan, 3, 2, 9, 1, 3, 0) == 16 && hga_attend_shared_workspace(&plan, 3, 2, 9, 1, 4, 0) == 64);
     for (int hint : {0, 1, 9, 10, INT_MAX}) {
         px.shared_hint = px.own_hint = hint;
         EXPECT(attend() == HGA_OK);

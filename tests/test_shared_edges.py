@@ -76,8 +76,8 @@ def test_values_that_are_no_numbers(hga, dtype, d, kv, ratio, n):
         px = P.prefixes(hga, seq, {s: 0 for s in range(n)}, [pages], sc.rng)
         ref, rlse, mag, reach, count = U.attend(f64(q), *clean, sc.table, seq, pos, kv, None, sc.n_ids)
         tol, ltol = P.attend_tolerance(sc, ref, mag, reach, count, clean[1], seq, pos)
-        for ws in (True, 0):
-            out, lse = P.attend(sc, batch, px, q, workspace=ws)
+        for share in (True, "few", False):
+            out, lse = P.attend(sc, batch, px, q, share=share)
             o = f64(out)
             assert np.array_equal(np.isnan(o), want)
             err, lerr = (np.abs(o - ref) / tol)[~want].max(), (np.abs(f64(lse) - rlse) / ltol).max()
@@ -155,7 +155,7 @@ def test_long_prefixes_with_absent_stretches(hga, dtype, d, kv, ratio, n):
         q = sc.random(n + 1, sc.hq, d)
         for hint in (None, 1, 9, 2 ** 31 - 1):
             px = P.prefixes(hga, seq, {s: 0 for s in range(n)}, [pages], sc.rng, hint)
-            P.check_attend(sc, q, P.attend(sc, batch, px, q))
+            P.check_attend(sc, q, P.attend(sc, batch, px, q, share=hint != 9))
 
 
 @pytest.mark.parametrize("dtype,d,kv,ratio,n", SHAPES)
@@ -176,6 +176,9 @@ def test_idle_tokens_in_groups(hga, dtype, d, kv, ratio, n):
         order = np.concatenate([order[order != n], [n]])
         px = hga.Prefixes(P.i32(order), P.i32([0, T - 1]), P.i32([pages]), pages, 2)
         out, lse = P.attend(sc, batch, px, q)
+        assert (f64(out)[n + 1:] == 0).all() and (f64(lse)[n + 1:] == -np.inf).all()
+        P.check_attend(sc, q, (out, lse), tokens=real)
+        out, lse = P.attend(sc, batch, px, q, share="few")
         assert (f64(out)[n + 1:] == 0).all() and (f64(lse)[n + 1:] == -np.inf).all()
         P.check_attend(sc, q, (out, lse), tokens=real)
     # nothing but idle ones; no sequences, no pages in the table
@@ -207,10 +210,10 @@ def test_groups_that_are_none(hga):
                                 (np.arange(21), [30, -5, 7], [big, -big]), (np.arange(21), [5, 5, 5], [1, 2]),
                                 (np.arange(21), [-big, big, 3, 12], [big, big, 6])):
         out = torch.full((23, sc.hq, 64), 5.0, dtype=torch.bfloat16, device="cuda")
-        px = hga.Prefixes(P.i32(order), P.i32(begin), P.i32(pages))
-        nb = hga.hga_attend_shared_workspace(sc.plan, batch, px)
+        b2, px = P.sharing(sc, batch, hga.Prefixes(P.i32(order), P.i32(begin), P.i32(pages)))
+        nb = hga.hga_attend_shared_workspace(sc.plan, b2, px)
         ws = torch.full((nb + 64,), 7, dtype=torch.uint8, device="cuda")
-        hga.hga_attend_shared(sc.plan, sc.pool, 0, batch, px, q, out[1:22], workspace=ws[:nb])
+        hga.hga_attend_shared(sc.plan, sc.pool, 0, b2, px, q, out[1:22], workspace=ws[:nb])
         torch.cuda.synchronize()
         assert (out[0] == 5).all() and (out[22] == 5).all() and (ws[nb:] == 7).all()
     assert np.array_equal(before, sc.stored())
@@ -227,12 +230,13 @@ def test_streams_and_replayed_graphs(hga, dtype, d, kv, ratio, n):
     seq = np.arange(n + 1)
     batch = sc.batch(seq, [min(sc.lens[s] - 1, PAGE * pages) for s in seq])
     q = sc.random(n + 1, sc.hq, d)
-    px = P.prefixes(hga, seq, {s: 0 for s in range(n)}, [pages], sc.rng, own_hint=2)
+    plain = P.prefixes(hga, seq, {s: 0 for s in range(n)}, [pages], sc.rng, own_hint=2)
+    batch, px = P.sharing(sc, batch, plain)
     length, budget = batch.tok_pos + 1, torch.full((n + 1,), 30, dtype=torch.int32, device="cuda")
 
     def state():
         f = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
-        st = dict(out=torch.zeros_like(q), lse=f(n + 1, sc.hq), w=f(n + 1, kv, sc.max_pages),
+        st = dict(out=torch.zeros_like(q), lse=f(n + 1, sc.hq), w=f(n + 1, kv, batch.max_pages),
                   ev=f(n + 1, 15, t=torch.int32))
         for name, nb in (("a", hga.hga_attend_shared_workspace(sc.plan, batch, px)),
                          ("b", hga.hga_weigh_pages_workspace(sc.plan, batch)),

@@ -57,12 +57,13 @@ def test_groups_of_every_kind(hga, dtype, d, kv, ratio):
     got = P.attend(sc, batch, px, q)
     P.check_attend(sc, q, got)
     assert _same(got, P.attend(sc, batch, px, q))
-    nb = hga.hga_attend_shared_workspace(sc.plan, batch, px)
-    for part in (0, 16, nb // 2 // 16 * 16, nb + 4096):
+    for part in (0, 16, 0.3, 0.6, 1.2):
         P.check_attend(sc, q, P.attend(sc, batch, px, q, workspace=part))
+    P.check_attend(sc, q, P.attend(sc, batch, px, q, share=False))
     # hints of any value, wrong ones among them
     for hint, own in ((0, 0), (1, 1), (3, 2), (2 ** 31 - 1, 7)):
-        P.check_attend(sc, q, P.attend(sc, batch, P.prefixes(hga, seq, group, pages, sc.rng, hint, own), q))
+        for share in (False, True):
+            P.check_attend(sc, q, P.attend(sc, batch, P.prefixes(hga, seq, group, pages, sc.rng, hint, own), q, share=share))
     # groups that share no page, and no groups
     P.check_attend(sc, q, P.attend(sc, batch, P.prefixes(hga, seq, group, [0, 0, 0, -3], sc.rng), q))
     P.check_attend(sc, q, P.attend(sc, batch, P.prefixes(hga, seq, {}, [], sc.rng), q))
@@ -81,10 +82,11 @@ def test_samples_of_one_prompt(hga, dtype, d, kv, ratio, n, pages):
     batch = sc.batch(seq, pos)
     q = sc.random(n, sc.hq, d)
     px = P.prefixes(hga, seq, {s: 0 for s in range(n)}, [pages], sc.rng, own_hint=5)
-    got = P.attend(sc, batch, px, q)
     some = slice(None) if n < 40 else slice(0, 40)
-    P.check_attend(sc, q, got, tokens=some)
-    assert _same(got, P.attend(sc, batch, px, q))
+    for share in (True, "few"):
+        got = P.attend(sc, batch, px, q, share=share)
+        P.check_attend(sc, q, got, tokens=some)
+        assert _same(got, P.attend(sc, batch, px, q, share=share))
 
 
 @pytest.mark.parametrize("dtype,d,kv,ratio,new", [("bf16", 128, 2, 8, 40), ("f32", 64, 2, 3, 5), ("bf16", 64, 1, 1, 70),
@@ -103,12 +105,28 @@ def test_drafts_and_questions_after_one_prompt(hga, dtype, d, kv, ratio, new):
         batch = sc.batch(seq[o], pos[o])
         q = sc.random(len(seq), sc.hq, d)
         px = P.prefixes(hga, seq[o], group, [pages], sc.rng)
-        P.check_attend(sc, q, P.attend(sc, batch, px, q))
+        for share in (True, "few"):
+            P.check_attend(sc, q, P.attend(sc, batch, px, q, share=share))
         # slots in the batch's own order
         of = np.array([0 if s in group else 1 for s in seq[o]])
         order = np.argsort(of, kind="stable")
         px = hga.Prefixes(P.i32(order), P.i32([0, int((of == 0).sum())]), P.i32([pages]), pages, 3)
         P.check_attend(sc, q, P.attend(sc, batch, px, q))
+
+
+@pytest.mark.parametrize("dtype,d,kv,ratio", [("bf16", 128, 2, 8), ("f32", 64, 2, 2), ("bf16", 64, 4, 1)])
+def test_hints_that_are_wrong(hga, dtype, d, kv, ratio):
+    """Prefixes longer and shorter than the host said, own pages too, where the
+    call shares."""
+    n = 60
+    for pages, hint, own in ((150, 80, 1), (150, 151, 40), (60, 152, 2), (90, 90, 1), (3, 140, 1)):
+        sc = _samples(hga, dtype, d, kv, ratio, n, pages, 400, seed=hint, max_pages=160)
+        seq = sc.rng.permutation(n)
+        batch = sc.batch(seq, [sc.lens[s] - 1 for s in seq])
+        q = sc.random(n, sc.hq, d)
+        px = P.prefixes(hga, seq, {s: 0 for s in range(n)}, [pages], sc.rng, hint, own)
+        for share in (False, True):
+            P.check_attend(sc, q, P.attend(sc, batch, px, q, share=share), tokens=slice(0, 25))
 
 
 def test_absent_and_cold_pages(hga):

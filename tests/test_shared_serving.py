@@ -129,18 +129,18 @@ def test_a_captured_step_over_shared_pages(hga):
     from paper_2606_30709_amd.pipeline import TokenPipeline
     plan = hga.Plan(batch=1, n_q_heads=8, n_kv_heads=2, head_dim=128, keep_first=1, keep_last=1, topk_chunks=3,
                     topk_groups=4)
-    cache = PagedCache(plan, 200, 9, 60, n_layers=1)
+    cache = PagedCache(plan, 260, 24, 160, n_layers=1)
     pipe, other = TokenPipeline(cache, False), TokenPipeline(cache, False)
     g = torch.Generator().manual_seed(4)
     rand = lambda *s: torch.randn(*s, generator=g).bfloat16().cuda()  # noqa: E731
-    pipe.step(0, cache.append([0], [64 * 30 + 5]), rand(1925, 8, 128), rand(1925, 2, 128), rand(1925, 2, 128))
-    for s in range(1, 9):
+    pipe.step(0, cache.append([0], [64 * 145 + 5]), rand(9285, 8, 128), rand(9285, 2, 128), rand(9285, 2, 128))
+    for s in range(1, 24):   # (so many that sharing pays)
         cache.fork(0, s)
-    seqs, ones = list(range(9)), [1] * 9
+    seqs, ones = list(range(24)), [1] * 24
     batch = cache.append(seqs, ones)
     px = cache.prefixes(batch, seqs, ones)
-    q, k, v = rand(9, 8, 128), rand(9, 2, 128), rand(9, 2, 128)
-    w, w2 = (torch.zeros(9, 2, 60, device="cuda") for _ in range(2))
+    q, k, v = rand(24, 8, 128), rand(24, 2, 128), rand(24, 2, 128)
+    w, w2 = (torch.zeros(24, 2, 160, device="cuda") for _ in range(2))
     pipe.step(0, batch, q, k, v, px, w)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
