@@ -997,8 +997,8 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
         c.run[i] = static_cast<int>(up(pages[i], c.most[i]));
     }
     // Own pages by a wavefront or a workgroup: what a round of workgroups takes, in pages, about five of them for what comes
-    // before the first (116 tokens of 8 heads, up to 10 pages: 27 us by wavefronts, 35 by workgroups; 64 of 4, up to 32, by
-    // workgroups 60, by wavefronts 71).
+    // before the first (256 tokens of 8 heads d64 with 20 own pages: 59 us a call by wavefronts, 73 by workgroups; 64 sequences
+    // of four tokens and 8 pages, 4 heads: 45 and 40).
     const int64_t own = static_cast<int64_t>(c.units[1]) * kv;
     c.alone = c.most[1] == 1 && up(own, 2 * kWaves * cus) * (5 + pages[1]) <= up(own, 2 * cus) * (5 + up(pages[1], kWaves));
     const int64_t counts = pad16(static_cast<int64_t>(n_tokens) * 8);
