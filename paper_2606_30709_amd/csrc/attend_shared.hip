@@ -32,6 +32,9 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // with one product where two bf16 terms need two.  Weights reach 2^kTop, 2^kLead when a reference is set: what lies below
 // 2^-24 in f16, 2^-35 of the column's largest weight, counts as none.  fp32 calls take three bf16 terms throughout.
 constexpr float kTop = 15.0f, kLead = 11.0f;
+// References from here on are off by more than kTop - kLead in their last place: the largest weight may pass 2^kTop, and f16's
+// end.  Columns with such a one go on in bf16 terms.
+constexpr float kFar = 0x1p27f;
 
 __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -56,6 +59,7 @@ struct ScaleRange {
             all &= w;
         }
     }
+    __device__ __forceinline__ void none() { any = ~0u; }
     __device__ __forceinline__ bool fits() const {
         return !__builtin_amdgcn_ballot_w64((any & 0x60606060u) != 0 || (~all & 0x80808080u) != 0);
     }
@@ -78,27 +82,29 @@ __device__ __forceinline__ void largest(const f32x4 (&sc)[kTiles][4], float (&to
             for (int x = 0; x < 4; ++x) top[i] = fmaxf(top[i], sc[i][tt][x]);
     }
 }
-// The running reference of every column, raised where a lane's scores exceed it by more than the slack.
-template <int D, int kTiles>
-__device__ __forceinline__ void raise_reference(const float (&tops)[kTiles], float scale, Acc<D, kTiles>& acc) {
+// The running reference of every column, raised where a lane's scores exceed it by more than the slack, compared as the
+// weights' exponents are formed: rounded once.  far(): some column's is kFar or more now.
+template <int D, int kTiles, typename F>
+__device__ __forceinline__ void raise_reference(const float (&tops)[kTiles], float scale, Acc<D, kTiles>& acc, F far) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(tops[i] * scale > acc.m[i] + kTop) != 0, 0)) {
-            const float top = max_groups(tops[i]) * scale;
-            const bool grow = top > acc.m[i] + kTop;
-            const float to = top - kLead;
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(fmaf(tops[i], scale, -acc.m[i]) > kTop) != 0, 0)) {
+            const float top = max_groups(tops[i]);
+            const bool grow = fmaf(top, scale, -acc.m[i]) > kTop;
+            const float to = fmaf(top, scale, -kLead);
             const float alpha = grow ? __builtin_amdgcn_exp2f(acc.m[i] - to) : 1.f;
             if (grow) acc.m[i] = to;
+            if (__builtin_amdgcn_ballot_w64(grow && !(fabsf(to) < kFar))) far();
             acc.l[i] *= alpha;
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) acc.o[i][j] *= alpha;
         }
 }
-template <int D, int kTiles>
-__device__ __forceinline__ void raise_reference(const f32x4 (&sc)[kTiles][4], float scale, Acc<D, kTiles>& acc) {
+template <int D, int kTiles, typename F>
+__device__ __forceinline__ void raise_reference(const f32x4 (&sc)[kTiles][4], float scale, Acc<D, kTiles>& acc, F far) {
     float top[kTiles];
     largest<kTiles>(sc, top);
-    raise_reference<D, kTiles>(top, scale, acc);
+    raise_reference<D, kTiles>(top, scale, acc, far);
 }
 
 template <int... kAt, typename F>
@@ -424,6 +430,7 @@ __device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensV
 
     Acc<D, 1> acc;
     clear(acc);
+    bool far = false;
     for (int e0 = run.a + wave; e0 < to; e0 += 64 * kTeam) {
         // the next 64 pages of this wavefront, one a lane
         SeenPage mine{-1, 0};
@@ -457,8 +464,8 @@ __device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensV
                 hide_rows<1>(seen, g, sc);
                 take_out_nan<D, 1>(v, m, g, seen, acc);
             }
-            raise_reference<D, 1>(sc, scale, acc);
-            by_terms<T>(values_fit(v.s), [&](auto half, auto terms) {
+            raise_reference<D, 1>(sc, scale, acc, [&] { far = true; });
+            by_terms<T>(!far && values_fit(v.s), [&](auto half, auto terms) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     float vs[2][4];
@@ -603,7 +610,8 @@ __device__ __forceinline__ void load_value_scales(buf_rsrc r, int m, int g, uint
 // SIMD.  16 questions of 128 tokens after 16K: 814 us with each wavefront decoding for itself, 640 through LDS, 583 with what
 // is rare outside the loop (its registers made the loop spill), 543 with the products beside the weights.  Four tiles a
 // wavefront, one wavefront a SIMD: 1,777 (spills); eight wavefronts to a page: 607 (a barrier's phases meet).
-// Only for columns that see all of the run, and for a bf16 call values that fit f16; false: they do not, nothing is stored.
+// Only for columns that see all of the run, and for a bf16 call values that fit f16 and references below kFar; false: they do
+// not, nothing is stored.
 template <typename T, int D, int kTiles>
 __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensView& tok, const PrefixView& px,
                                             const SharedArgs& a, const T* __restrict__ q, int64_t q_stride, float* smem, int h,
@@ -614,7 +622,7 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(D));  // log2(e) / sqrt(d)
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, m = lane & 15, g = lane >> 4;
     u32x4* const pages = reinterpret_cast<u32x4*>(smem);                // [2][kFrags][64]
-    int* const s_of = reinterpret_cast<int*>(smem + 2 * kFrags * 256);  // [wave][2]
+    int* const s_of = reinterpret_cast<int*>(smem + 2 * kFrags * 256);  // [wave][2], then [wave]
     const int columns = n_slots * a.ratio, c0 = wave * 16 * kTiles, heads = pool.n_kv * a.ratio;
 
     Columns<T, D, kTiles> col;
@@ -713,7 +721,7 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
         for (bool more = true; more;) {
             u32x4* const page = pages + bit * kFrags * 64;
             u32x4* const other = pages + (bit ^ 1) * kFrags * 64;
-            raise_reference<D, kTiles>(top, scale, acc);
+            raise_reference<D, kTiles>(top, scale, acc, [&] { range.none(); });
             u32x4 w[2][kTiles][kParts], kf[2][kSteps];
             float base[kTiles];
 #pragma unroll
@@ -792,7 +800,16 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
             __syncthreads();
         }
     }
-    if (kHalf && !range.fits()) return false;
+    if constexpr (kHalf) {
+        // (the references are each wavefront's own)
+        const bool fits = range.fits();
+        if (lane == 0) s_of[2 * kWaves + wave] = fits;
+        __syncthreads();
+        int all = 1;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all &= s_of[2 * kWaves + w];
+        if (!__builtin_amdgcn_readfirstlane(all)) return false;
+    }
     // columns of no token saw the pages too
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
@@ -1019,7 +1036,7 @@ template <typename T, int D, int kTiles>
 hipError_t run(const hga_plan& plan, const PoolView& pool, const TokensView& tok, const PrefixView& px, const SharedArgs& a,
                const void* q, int64_t q_stride, void* out, hipStream_t stream) {
     constexpr size_t kJoin = sizeof(float) * kWaves * 16 * (D + 4 + 2);
-    constexpr size_t kPages = kTiles ? 2 * (D / 4) * 1024 + 2 * kWaves * 4 : 0;
+    constexpr size_t kPages = kTiles ? 2 * (D / 4) * 1024 + 3 * kWaves * 4 : 0;
     constexpr size_t lds = std::max(kJoin, kPages);
     const auto kernel = attend_shared_kernel<T, D, kTiles>;
     hipError_t e;
