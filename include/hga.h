@@ -823,7 +823,10 @@ int64_t hga_weigh_pages_workspace(const hga_plan* plan, int32_t n_tokens, int32_
  *   workspace   hga_weigh_pages_workspace bytes, or NULL and 0 (a call of many
  *               tokens of few pages then takes longer); calls that overlap in
  *               time need one each.  Its size decides the order of sums.
- * Sums are held in fp32 and do not depend on anything that runs beside them. */
+ * Sums are held in fp32 and do not depend on anything that runs beside them.
+ * Weights go by row of the table and chunk: a caller that gives a row, or the
+ * chunks behind a cut, to other tokens clears theirs, and copies a row's for a
+ * sequence that goes on from it. */
 hga_status hga_weigh_pages(const hga_plan* plan, const hga_pool* pool, int32_t layer,
                            const hga_tokens* tokens, const void* q, int64_t q_stride,
                            const float* lse, const int32_t* chunk_list, int32_t n_list,

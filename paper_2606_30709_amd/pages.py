@@ -239,7 +239,7 @@ class PagedCache:
 
     ``append`` gives the batch of the next tokens, which ``hga_cache_append``
     then stores layer by layer; ``page_table`` (int32 [n_seqs, max_pages], on
-    the GPU) is updated in place."""
+    the GPU) is updated in place, and so is what ``page_weights`` gave."""
 
     def __init__(self, plan: hga.Plan, n_pages: int, n_seqs: int, max_pages: int, n_layers: int = 1,
                  n_cold: int = 0, device="cuda"):
@@ -248,6 +248,24 @@ class PagedCache:
         self.pool = hga.Pool(plan, n_pages, n_layers, n_cold, device)
         self.page_table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32,
                                      device=self.pool.device)
+        self._weights = None
+
+    def page_weights(self) -> torch.Tensor:
+        """The cache's own attention weights of pages, fp32 [n_layers, n_seqs,
+        n_kv_heads, max_pages], zeros before the first call, the same tensor in
+        every call: ``TokenPipeline.step`` adds a layer's to it, ``evict`` goes by
+        its sum over layers, or one layer.  They go with their sequences: ``fork``
+        copies them, ``release`` clears them, ``truncate`` those of the chunks it
+        drops (a chunk that it cuts keeps what the chunk had).  In a tensor of the
+        caller's own that is left to the caller: without it a row's next sequence
+        goes on from the last one's weights."""
+        if self._weights is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise hga.HgaError(-1, "HGA_EINVAL: the page weights of a captured step have to be there before it")
+            p = self.plan.params
+            self._weights = torch.zeros(self.pool.n_layers, len(self.book.length), p.n_kv_heads, self.book.max_pages,
+                                        dtype=torch.float32, device=self.pool.device)
+        return self._weights
 
     def length(self, s: int) -> int:
         return int(self.book.length[s])
@@ -317,9 +335,9 @@ class PagedCache:
     def evict(self, weights: torch.Tensor, budget) -> list:
         """Drop of each sequence s the pages above budget[s] (an int: of every one)
         that hga_choose_evictions names by ``weights`` (fp32 [n_seqs, n_kv_heads,
-        max_pages]: those of one layer, or a sum over them); the chunks dropped,
-        a list for each sequence.  Waits for the device; the weights are not
-        changed (an absent page gets nothing more)."""
+        max_pages]: those of one layer, or a sum over them, see ``page_weights``);
+        the chunks dropped, a list for each sequence.  Waits for the device; the
+        weights are not changed (an absent page gets nothing more)."""
         book = self.book
         n_seqs = len(book.length)
         want = np.broadcast_to(np.asarray(budget, np.int64), (n_seqs,))
@@ -345,14 +363,25 @@ class PagedCache:
         """As PageBook.truncate; so the methods that follow."""
         self.book.truncate(s, length)
         self._apply(None)
+        self._forget(s, -(-length // PAGE))
 
     def release(self, s: int):
         self.book.release(s)
         self._apply(None)
+        self._forget(s, 0)
 
     def fork(self, src: int, dst: int):
         self.book.fork(src, dst)
         self._apply(None)
+        if self._weights is not None and src != dst:
+            with torch.cuda.device(self.pool.index):
+                self._weights[:, dst] = self._weights[:, src]
+
+    def _forget(self, s: int, begin: int):
+        """The page weights of sequence s from chunk `begin` on become zeros."""
+        if self._weights is not None:
+            with torch.cuda.device(self.pool.index):
+                self._weights[:, s, :, begin:].zero_()
 
     def drop(self, s: int, begin: int, end: int):
         self.book.drop(s, begin, end)

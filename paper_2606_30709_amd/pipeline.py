@@ -566,8 +566,9 @@ class TokenPipeline:
         out (as q) and lse fp32 [n_tokens, n_q_heads], valid until the next
         step.  prefixes (``PagedCache.prefixes``; without routing): the pages
         that the batch's sequences share.  weights fp32 [n_seqs, n_kv_heads,
-        max_pages]: the pages' attention weight, added to (``PagedCache.evict``
-        takes it).  Runs on the current stream."""
+        max_pages]: the pages' attention weight, added to (a layer's of
+        ``PagedCache.page_weights``, which keeps them with their sequences;
+        ``PagedCache.evict`` takes it).  Runs on the current stream."""
         p, plan, pool = self.plan.params, self.plan, self.cache.pool
         T = batch.n_tokens
         # every buffer before the first launch
