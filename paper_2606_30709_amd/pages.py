@@ -241,6 +241,8 @@ class PagedCache:
     then stores layer by layer; ``page_table`` (int32 [n_seqs, max_pages], on
     the GPU) is updated in place, and so is what ``page_weights`` gave."""
 
+    _weights = None  # what page_weights gave
+
     def __init__(self, plan: hga.Plan, n_pages: int, n_seqs: int, max_pages: int, n_layers: int = 1,
                  n_cold: int = 0, device="cuda"):
         self.plan = plan
@@ -248,7 +250,6 @@ class PagedCache:
         self.pool = hga.Pool(plan, n_pages, n_layers, n_cold, device)
         self.page_table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32,
                                      device=self.pool.device)
-        self._weights = None
 
     def page_weights(self) -> torch.Tensor:
         """The cache's own attention weights of pages, fp32 [n_layers, n_seqs,
