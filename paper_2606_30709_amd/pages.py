@@ -334,21 +334,22 @@ class PagedCache:
         return hga.Prefixes(order, begin, shared, max(p for _, p in groups), max(own, 1))
 
     def evict(self, weights: torch.Tensor, budget) -> list:
-        """Drop of each sequence s the pages above budget[s] (an int: of every one)
-        that hga_choose_evictions names by ``weights`` (fp32 [n_seqs, n_kv_heads,
-        max_pages]: those of one layer, or a sum over them, see ``page_weights``);
-        the chunks dropped, a list for each sequence.  Waits for the device; the
-        weights are not changed (an absent page gets nothing more)."""
+        """Drop of each sequence s the pages above budget[s] (an int: of every one;
+        one below 0 counts as 0) that hga_choose_evictions names by ``weights``
+        (fp32 [n_seqs, n_kv_heads, max_pages]: those of one layer, or a sum over
+        them, see ``page_weights``); the chunks dropped, a list for each sequence.
+        Waits for the device; the weights are not changed (an absent page gets
+        nothing more)."""
         book = self.book
         n_seqs = len(book.length)
-        want = np.broadcast_to(np.asarray(budget, np.int64), (n_seqs,))
+        want = np.broadcast_to(np.asarray(budget, np.int64), (n_seqs,)).clip(0, 2 ** 31 - 1)
         here = (book.table >= 0).sum(1)
         most = int((here - want).clip(0).max(initial=0))
         if most == 0:
             return [[] for _ in range(n_seqs)]
         dev = self.pool.device
         with torch.cuda.device(self.pool.index):
-            state = self._upload(np.stack((book.length, want.clip(0, 2 ** 31 - 1))).astype(np.int32))
+            state = self._upload(np.stack((book.length, want)).astype(np.int32))
             out = torch.empty(n_seqs, most, dtype=torch.int32, device=dev)
             nbytes = hga.hga_choose_evictions_workspace(self.plan, self.page_table)
             ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
