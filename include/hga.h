@@ -798,7 +798,9 @@ hga_status hga_attend_shared(const hga_plan* plan, const hga_pool* pool, int32_t
  * A cache that has outgrown its pool gives up the pages that attention made
  * least use of: hga_weigh_pages sums up what each page got, token after token,
  * hga_choose_evictions names those to drop, and their table entries then mark
- * absent pages. */
+ * absent pages.  Each row is chosen from by its own weights: a page that several
+ * rows name is free when all of them have dropped it, which rows agree on whose
+ * weights of such pages are the sums over all of them. */
 
 /* Bytes of workspace hga_weigh_pages makes use of (n_list 0: every chunk), or a
  * negative hga_status.  Host only. */

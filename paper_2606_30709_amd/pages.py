@@ -333,13 +333,20 @@ class PagedCache:
         order, begin, shared = up.split((batch.n_tokens, len(groups) + 1, len(groups)))
         return hga.Prefixes(order, begin, shared, max(p for _, p in groups), max(own, 1))
 
-    def evict(self, weights: torch.Tensor, budget) -> list:
+    def evict(self, weights: torch.Tensor, budget, together: bool = False) -> list:
         """Drop of each sequence s the pages above budget[s] (an int: of every one;
         one below 0 counts as 0) that hga_choose_evictions names by ``weights``
         (fp32 [n_seqs, n_kv_heads, max_pages]: those of one layer, or a sum over
         them, see ``page_weights``); the chunks dropped, a list for each sequence.
         Waits for the device; the weights are not changed (an absent page gets
-        nothing more)."""
+        nothing more).
+
+        A page that sequences share is free only when all of them have dropped it,
+        and those that drop different pages begin with fewer in common
+        (``prefixes``).  Each sequence by itself chooses by its own weights;
+        together: a page counts in all of its sequences by what it got of all of
+        them, so that forks drop the same pages of their prompt, one with a smaller
+        budget (or a shorter window) those and the next ones."""
         book = self.book
         n_seqs = len(book.length)
         want = np.broadcast_to(np.asarray(budget, np.int64), (n_seqs,)).clip(0, 2 ** 31 - 1)
@@ -351,6 +358,8 @@ class PagedCache:
         with torch.cuda.device(self.pool.index):
             state = self._upload(np.stack((book.length, want)).astype(np.int32))
             out = torch.empty(n_seqs, most, dtype=torch.int32, device=dev)
+            if together:
+                weights = self._of_sharers(weights)
             nbytes = hga.hga_choose_evictions_workspace(self.plan, self.page_table)
             ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
             hga.hga_choose_evictions(self.plan, self.page_table, book.n_pages + book.n_cold, state[0], weights,
@@ -360,6 +369,25 @@ class PagedCache:
             book.evict(s, chunks)
         self._apply(None)
         return chosen
+
+    def _of_sharers(self, weights: torch.Tensor) -> torch.Tensor:
+        """weights, a page's that sequences share the sum of theirs: in 64 bits, a
+        sequence at a time, so that it is the same in each of them and every time."""
+        book, kv = self.book, self.plan.params.n_kv_heads
+        hga._expect(weights, "weights", torch.float32, (*book.table.shape[:1], kv, book.max_pages), self.pool.device)
+        rows, chunks = np.nonzero((book.table >= 0) & (book.refs[book.table] > 1))
+        if not len(rows):
+            return weights
+        at = self._upload(np.stack((chunks, book.table[rows, chunks])).astype(np.int64))
+        counts = np.bincount(rows, minlength=len(book.length)).tolist()
+        parts = [(s, *x) for s, x in enumerate(zip(*(y.split(counts) for y in at))) if counts[s]]
+        total = torch.zeros(kv, book.n_pages + book.n_cold, dtype=torch.float64, device=weights.device)
+        for s, c, page in parts:     # (no page stands twice in a row)
+            total[:, page] += weights[s][:, c].double()
+        weights = weights.clone()
+        for s, c, page in parts:
+            weights[s].index_copy_(1, c, total[:, page].float())
+        return weights
 
     def truncate(self, s: int, length: int):
         """As PageBook.truncate; so the methods that follow."""
