@@ -59,15 +59,30 @@ struct ScaleRange {
             all &= w;
         }
     }
-    __device__ __forceinline__ void none() { any = ~0u; }
     __device__ __forceinline__ bool fits() const {
         return !__builtin_amdgcn_ballot_w64((any & 0x60606060u) != 0 || (~all & 0x80808080u) != 0);
     }
 };
-__device__ __forceinline__ bool values_fit(const uint32_t (&s)[4]) {
+// Zeros fit whatever their scale (a block of zeros is stored with the smallest one), unless they stand for NaN: whether rows
+// whose scales do not fit hold nothing else in any lane's dimensions.
+template <int D>
+__device__ __forceinline__ bool zeros_fit(const Values<D>& v) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const uint32_t e = v.s[t] >> (8 * x) & 255u;
+            const uint32_t codes = D == 128 ? v.c[t][x % (D / 32)] : v.c[t][x / 2] >> (16 * (x % 2)) & 0xffffu;
+            bad |= e - 109u > 31u ? (codes & 0x77777777u) | static_cast<uint32_t>(e == 255u) : 0u;
+        }
+    return !__builtin_amdgcn_ballot_w64(bad != 0);
+}
+template <int D>
+__device__ __forceinline__ bool values_fit(const Values<D>& v) {
     ScaleRange r;
-    r.add(s);
-    return r.fits();
+    r.add(v.s);
+    return __builtin_expect(r.fits(), 1) || zeros_fit<D>(v);
 }
 
 // The largest of a lane's scores.
@@ -465,7 +480,7 @@ __device__ __forceinline__ void attend_slots(const PoolView& pool, const TokensV
                 take_out_nan<D, 1>(v, m, g, seen, acc);
             }
             raise_reference<D, 1>(sc, scale, acc, [&] { far = true; });
-            by_terms<T>(!far && values_fit(v.s), [&](auto half, auto terms) {
+            by_terms<T>(sizeof(T) == 2 && !far && values_fit<D>(v), [&](auto half, auto terms) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     float vs[2][4];
@@ -610,8 +625,10 @@ __device__ __forceinline__ void load_value_scales(buf_rsrc r, int m, int g, uint
 // SIMD.  16 questions of 128 tokens after 16K: 814 us with each wavefront decoding for itself, 640 through LDS, 583 with what
 // is rare outside the loop (its registers made the loop spill), 543 with the products beside the weights.  Four tiles a
 // wavefront, one wavefront a SIMD: 1,777 (spills); eight wavefronts to a page: 607 (a barrier's phases meet).
+// At d128 bf16 it holds 256 registers and spills 96 bytes a lane, none of which the loop over pages touches (but for its branch
+// that raises a reference).
 // Only for columns that see all of the run, and for a bf16 call values that fit f16 and references below kFar; false: they do
-// not, nothing is stored.
+// not (looked at every 64 pages), nothing is stored.
 template <typename T, int D, int kTiles>
 __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensView& tok, const PrefixView& px,
                                             const SharedArgs& a, const T* __restrict__ q, int64_t q_stride, float* smem, int h,
@@ -622,7 +639,7 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
     const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(D));  // log2(e) / sqrt(d)
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, m = lane & 15, g = lane >> 4;
     u32x4* const pages = reinterpret_cast<u32x4*>(smem);                // [2][kFrags][64]
-    int* const s_of = reinterpret_cast<int*>(smem + 2 * kFrags * 256);  // [wave][2], then [wave]
+    int* const s_of = reinterpret_cast<int*>(smem + 2 * kFrags * 256);  // [wave][2], then [wave]: no reason to stop
     const int columns = n_slots * a.ratio, c0 = wave * 16 * kTiles, heads = pool.n_kv * a.ratio;
 
     Columns<T, D, kTiles> col;
@@ -631,9 +648,11 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) first = min(first, col.pos[i] < 0 ? INT32_MAX : col.pos[i]);
     first = -1 - row_max(-1 - first);
+    int* const s_fit = s_of + 2 * kWaves;
     if (lane == 0) {
         s_of[2 * wave] = col.s;
         s_of[2 * wave + 1] = first;
+        s_fit[wave] = 1;
     }
     __syncthreads();
 #pragma unroll
@@ -721,7 +740,7 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
         for (bool more = true; more;) {
             u32x4* const page = pages + bit * kFrags * 64;
             u32x4* const other = pages + (bit ^ 1) * kFrags * 64;
-            raise_reference<D, kTiles>(top, scale, acc, [&] { range.none(); });
+            raise_reference<D, kTiles>(top, scale, acc, [&] { s_fit[wave] = 0; });
             u32x4 w[2][kTiles][kParts], kf[2][kSteps];
             float base[kTiles];
 #pragma unroll
@@ -799,16 +818,27 @@ __device__ __forceinline__ bool attend_wide(const PoolView& pool, const TokensVi
             bit ^= 1;
             __syncthreads();
         }
-    }
-    if constexpr (kHalf) {
-        // (the references are each wavefront's own)
-        const bool fits = range.fits();
-        if (lane == 0) s_of[2 * kWaves + wave] = fits;
-        __syncthreads();
-        int all = 1;
+        if constexpr (kHalf) {
+            if (__builtin_expect(!range.fits(), 0)) {
+                // Zeros, perhaps: the pages' values once more, each wavefront a share of them (16 questions of 128 tokens after
+                // 16K, a row of zeros in every page or every 64th: 573 and 565 us, by few columns 1,476 and 1,321, without such
+                // rows 540; looked for page by page in the loop, that takes 561 without any).
+                const uint64_t pages_here = __builtin_amdgcn_ballot_w64(pool.has(id));
+                const int rank = __popcll(pages_here & ((uint64_t(1) << lane) - 1));
+                for (uint64_t mine = __builtin_amdgcn_ballot_w64(pool.has(id) && rank % kWaves == wave); mine; mine &= mine - 1) {
+                    Values<D> v;
+                    load_values<D, 0>(part(static_cast<int>(__builtin_ctzll(mine))), m, g, v);
+                    if (!zeros_fit<D>(v)) s_fit[wave] = 0;
+                }
+                range = ScaleRange();
+                __syncthreads();
+            }
+            // (written again behind the next pages' first barrier at the earliest)
+            int fit = 1;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) all &= s_of[2 * kWaves + w];
-        if (!__builtin_amdgcn_readfirstlane(all)) return false;
+            for (int w = 0; w < kWaves; ++w) fit &= s_fit[w];
+            if (!__builtin_amdgcn_readfirstlane(fit)) return false;
+        }
     }
     // columns of no token saw the pages too
 #pragma unroll
