@@ -329,9 +329,10 @@ __device__ __forceinline__ void load_columns(const PoolView& pool, const TokensV
     for (int i = 0; i < kTiles; ++i) {
         const int c = c0 + 16 * i + m;
         const bool real = c < columns;
-        const int t = real ? px.token(at + c / ratio, tok.n_tokens) : -1;
+        // (a column past the last has the last slot's query)
+        const int t = px.token(at + min(c, columns - 1) / ratio, tok.n_tokens);
         int sc = 0, pc = 0;
-        const bool in = t >= 0 && tok.at(t, sc, pc);
+        const bool there = t >= 0 && tok.at(t, sc, pc), in = real && there;
         r.pos[i] = in ? pc : -1;
         last = max(last, r.pos[i]);
         // columns past the last are no reason to look at rows one by one
@@ -351,6 +352,12 @@ __device__ __forceinline__ void load_columns(const PoolView& pool, const TokensV
                 for (int y = 0; y < kTerms; ++y) r.qf[i][y][kk][e] = w[y];
             }
         }
+        // an idle token's query may be anything, and would decide which types the others' products take
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!there) != 0, 0))
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk)
+#pragma unroll
+                for (int y = 0; y < kTerms; ++y) r.qf[i][y][kk] = there ? r.qf[i][y][kk] : u32x4{0u, 0u, 0u, 0u};
     }
     r.s = __builtin_amdgcn_readfirstlane(row_max(s));
     r.first = -1 - __builtin_amdgcn_readfirstlane(row_max(-1 - first));
@@ -625,7 +632,7 @@ __device__ __forceinline__ void load_value_scales(buf_rsrc r, int m, int g, uint
 // SIMD.  16 questions of 128 tokens after 16K: 814 us with each wavefront decoding for itself, 640 through LDS, 583 with what
 // is rare outside the loop (its registers made the loop spill), 543 with the products beside the weights.  Four tiles a
 // wavefront, one wavefront a SIMD: 1,777 (spills); eight wavefronts to a page: 607 (a barrier's phases meet).
-// At d128 bf16 it holds 256 registers and spills 96 bytes a lane, none of which the loop over pages touches (but for its branch
+// At d128 bf16 it holds 256 registers and spills 76 bytes a lane, none of which the loop over pages touches (but for its branch
 // that raises a reference).
 // Only for columns that see all of the run, and for a bf16 call values that fit f16 and references below kFar; false: they do
 // not (looked at every 64 pages), nothing is stored.

@@ -84,3 +84,26 @@ def test_scores_of_any_size(hga, dtype, d, kv, ratio, n, few, power):
                 rel = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -22
                 assert (np.abs(out[t, i] - want) <= rel * np.abs(want) + 2.0 ** -60).all()
     assert ahead >= n * sc.hq // 2 and 2.0 ** (power - 2) < largest < 2.0 ** 30.5
+
+
+@pytest.mark.parametrize("dtype,d,kv,ratio,n", [("bf16", 128, 2, 8, 30), ("bf16", 64, 1, 3, 60), ("bf16", 128, 1, 4, 3), ("f32", 64, 1, 1, 90)])
+@pytest.mark.parametrize("few", [False, "few"])
+def test_queries_of_idle_tokens_change_no_bit_of_the_others(hga, dtype, d, kv, ratio, n, few):
+    """Padding slots among a group's, whose queries are zeros, the largest numbers,
+    infinities or NaN."""
+    lens = [PAGE * 17 + 1 + i for i in range(n)]
+    sc = Scene(hga, dtype, d, kv, ratio, lens=lens, seed=n)
+    P.share(sc, [(0, list(range(1, n)), 17)])
+    seq = np.array([0, 1, -1, n, *range(n)])
+    pos = np.array([-1, 10 ** 7, 5, 5] + [x - 1 for x in lens])
+    batch = sc.batch(seq, pos)
+    order = sc.rng.permutation(n + 4)
+    px = hga.Prefixes(P.i32(order), P.i32([0, n + 4]), P.i32([17]), 17, 2)
+    q = sc.random(n + 4, sc.hq, d)
+    got = []
+    for x in (0.0, torch.finfo(q.dtype).max, -torch.finfo(q.dtype).max, float("inf"), float("nan")):
+        q[:4] = x
+        got.append(P.attend(sc, batch, px, q, share=few or True))
+        assert all(torch.equal(a, b) for a, b in zip(got[0], got[-1])), x
+    assert (got[0][0][:4] == 0).all() and (got[0][1][:4] == -float("inf")).all()
+    P.check_attend(sc, q, got[0], tokens=np.arange(4, n + 4, 4))
