@@ -778,7 +778,9 @@ int64_t hga_attend_shared_workspace(const hga_plan* plan, int32_t n_tokens, int3
 
 /* hga_attend_tokens over whole histories, each group's shared pages read once:
  * out and lse are what that call writes, up to the order of sums and, in bf16,
- * the rounding of the weights (to 11 bits here, a 2^-12 of each; to 16 there).
+ * the rounding of the weights (to 11 bits here: off by up to 2^-11 of each, or by
+ * 2^-35 of the token's largest where that is more; to 16 bits there, and here for
+ * values that f16 does not hold and scores from 2^24 / log2(e) on).
  * Where groups are so small, or share so little, that this takes longer than each
  * token by itself, it is that call.  Arguments, requirements and errors as there,
  * without lists;

@@ -9,8 +9,8 @@
 // own (4 times 32, or 16 in fp32 at 128 dimensions) and decode each page once for all of them, into LDS.  A unit's pages are cut into runs, a workgroup
 // each, so that some 512 are at work; a second kernel joins the runs' results in order.
 //
-// 64 samples of a 16K prompt (32/4 heads d128 bf16): 48 us; 16 questions of 128 tokens about 16K: 545 us (1.0 PFLOP/s; 1.9 us
-// a page, 1.14 PFLOP/s, as fast as a large matrix product here).
+// 64 samples of a 16K prompt (32/4 heads d128 bf16): 49 us; 16 questions of 128 tokens about 16K: 545 us (1.0 PFLOP/s; 1.9 us
+// a page, 1.14 PFLOP/s, 93 % of a large matrix product's rate here).
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -28,13 +28,14 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // A bf16 call's weights and values enter their product as f16.  A value is exact there: one code has two significant bits,
 // and pages with a scale outside 2^-18 .. 2^13 (where f16 would run out of bits, or overflow) take bf16 and its further terms
-// instead.  A weight has 11 bits, which leaves out 2^-12 of it at most where the result's own rounding to bf16 takes 2^-9,
-// with one product where two bf16 terms need two.  Weights reach 2^kTop, 2^kLead when a reference is set: what lies below
-// 2^-24 in f16, 2^-35 of the column's largest weight, counts as none.  fp32 calls take three bf16 terms throughout.
+// instead.  A weight has 11 bits, which leaves out 2^-11 of it at most where the result's own rounding to bf16 takes 2^-8,
+// with one product where two bf16 terms need two.  Weights reach 2^kTop, 2^kLead when a reference is set: f16 holds multiples
+// of 2^-24, so that a weight is off by up to 2^-35 of the column's largest where that is more, and one below that counts as
+// none.  fp32 calls take three bf16 terms throughout.
 constexpr float kTop = 15.0f, kLead = 11.0f;
-// References from here on are off by more than kTop - kLead in their last place: the largest weight may pass 2^kTop, and f16's
-// end.  Columns with such a one go on in bf16 terms.
-constexpr float kFar = 0x1p27f;
+// References from here on are off by 1 or more in their last place, and by so much the weights from where f16 holds them (from
+// 2^27 on the largest may pass its end).  Columns with such a one go on in bf16 terms.
+constexpr float kFar = 0x1p24f;
 
 __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -1115,8 +1116,10 @@ int64_t attend_shared_bytes(const hga_plan& plan, int n_tokens, int n_seqs, int 
 // as much as prefixes of up to 128 pages are long.  Measured over 1 and 8 groups of 2 to 128 sequences after 8 to 384 pages
 // (32/4 heads d128 and 8/8 d64 bf16, 16/4 d128 and 8/4 d64 fp32; 1 and 4 tokens each), us shared and not: 512 tile pages of
 // prefixes of 8 pages 8.9 and 6.1, 4,096 of 8 19.0 and 13.0, 2,048 of 32 12.1 and 11.5, 4,096 of 32 13.8 and 15.5, 16,384 of 8
-// 14.2 and 22.3, 4,096 of 128 14.2 and 16.4, 16,384 of 128 22.6 and 29.8, 65,536 of 32 20.4 and 51.3; above the border it is
-// longer by 7 us at most (16,384 of 32, drafts of four in fp32: 44.9 and 37.9).
+// 14.2 and 22.3, 4,096 of 128 14.2 and 16.4, 16,384 of 128 22.6 and 29.8, 65,536 of 32 20.4 and 51.3.  Own pages are not in the
+// rule, though what they take grows with the tokens: above the border drafts of four after 32 pages take longer shared, 8
+// groups of 32 sequences 94.7 and 82.1 (32/4 heads d128 bf16; one token each 30.7 and 41.1, after 128 pages 164 and 221), 67.8
+// and 62.9 (16/4 d128 fp32), one group of 128 41.5 and 34.4.
 bool attend_shared_pays(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int n_groups, int shared_hint) {
     if (n_groups == 0 || std::min(n_seqs, n_tokens) < 2 * static_cast<int64_t>(n_groups)) return false;
     const int64_t tiles = (static_cast<int64_t>(n_tokens) + own_slots(plan, n_tokens, n_seqs) - 1) / own_slots(plan, n_tokens, n_seqs);
