@@ -315,8 +315,11 @@ Cut cut_call(const hga_plan& plan, int n_tokens, int n_seqs, int max_pages, int 
         c.run = static_cast<int>(std::clamp<int64_t>(most, 1, 64));
         c.blocks = (max_pages + c.run * c.waves - 1) / (c.run * c.waves);
     }
-    // Slices of the tokens where the pages alone do not fill the device: of two tiles' tokens at least (32 tokens each of six
-    // sequences, 12 heads of d64: 20 us without, 15.5 with).
+    // Slices of the tokens where the pages alone do not fill the device: of two tiles' tokens at least.  us with and without:
+    // 512 tokens of one sequence of 1,024, 12 heads of d64 fp32, 16 slices 14.4 and 45.4; 256 of 2,048, 32/4 d128 bf16, 32 slices
+    // 27.6 and 155; 8 times 256 tokens of 31 listed pages, 16 slices 1,072 and 2,125.  Units, pages and tokens of a sequence are
+    // counted by the table's rows and width, as the host knows no better: in a table of many more, runs are longer and slices
+    // fewer than the batch would need.
     const int64_t have = units * c.blocks * c.waves;
     const int least = std::max(1, n_list ? 2 : 32 / ratio);
     const int per_seq = static_cast<int>((static_cast<int64_t>(n_tokens) + n_seqs - 1) / std::max(n_seqs, 1));

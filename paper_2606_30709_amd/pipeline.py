@@ -536,8 +536,9 @@ class TokenPipeline:
     may be captured into a graph; one that would have to allocate is refused
     while a stream captures.  What a captured step uses is kept for the
     pipeline's life, whatever larger steps come later: replays need the pipeline
-    (and the batch's tensors) alive, and the steps and replays of one pipeline
-    in an order, since they share its buffers."""
+    (and the tensors that the step was given, the batch's and the prefixes' too)
+    alive, and the steps and replays of one pipeline in an order, since they
+    share its buffers."""
 
     def __init__(self, cache, routed: bool = True):
         self.cache, self.plan, self.routed = cache, cache.plan, routed
